@@ -66,7 +66,11 @@ typedef enum {
 typedef enum {
   LA_F32 = 0,
   LA_BF16 = 1,
-  LA_FP8_E4M3 = 2                /* OCP e4m3fn: no infinities, max 448                 */
+  LA_FP8_E4M3 = 2,               /* OCP e4m3fn: no infinities, max 448                 */
+  /* rows of a block cache only (la_kv_store and what reads it): elements in groups of 32
+     along the head dimension that share a power of two, kept apart from the elements    */
+  LA_MXFP8_E4M3 = 3,             /* fp8-e4m3 elements                                  */
+  LA_MXFP4_E2M1 = 4              /* fp4-e2m1 elements, two to a byte, the even one low */
 } la_dtype;
 
 /* ------------------------------------------------------------------------- *
@@ -304,6 +308,128 @@ LA_API la_status la_kv_commit_tree(
     const float *k_scale, const float *v_scale,
     int32_t *new_prefix_lens,        /* dev [B], written                                           */
     const la_layer_strides *layers, void *hip_stream);
+
+/* ------------------------------------------------------------------------- *
+ *  Block cache: a paged K/V cache that is quantised as it is written and whose
+ *  blocks are chosen by their keys' bounds
+ *
+ *  Formats (la_attn_desc.kv_dtype of the calls below): LA_BF16, LA_MXFP8_E4M3,
+ *  LA_MXFP4_E2M1.  A quantised row of D elements is D / 32 groups; group x has
+ *  the exponent E, the smallest integer in [-100, 100] with
+ *  max |x_i| <= M * 2^E (M = 448 or 6; an all-zero group: -100), and element i
+ *  the code nearest to x_i * 2^-E, ties to even, saturating at +-M.  Its value
+ *  is code * 2^E, exact in bf16.  E is stored as the byte E + 127.
+ *
+ *  Beside the rows the cache may keep, per block and KV head, the smallest and
+ *  the largest stored key of every channel (k_bounds, bf16, exact).
+ *
+ *  la_kv_store appends rows as la_kv_commit does (chain, then a branch's own
+ *  tokens) and keeps the bounds: a block that begins with a new row gets the
+ *  bounds of its new rows, the block that the prefix ends in has its bounds
+ *  widened by them.  (Bounds are never narrowed: where a prefix is shortened
+ *  inside a block, they go on covering what was there.)  Single tokens, whole
+ *  prompts and drafted steps are one call: prompts of different lengths are a
+ *  batch of the longest with n_own[b] of its rows real.
+ *  la_kv_load brings rows back.  la_block_select lists blocks;
+ *  la_verify_attention_sparse attends to them.
+ *
+ *  head_dim 64 / 128 / 256; q and the branch's (chain's) K and V bf16.  A bf16
+ *  block cache is laid out as la_verify_attention's.  The other conventions are
+ *  the header's: what is not finite gives undefined values, block ids are
+ *  trusted, desc->kv_split_tokens and kernel_shape must be 0.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  void *k, *v;              /* dev [num_blocks, Hkv, block_size, D] elements, of layer 0           */
+  uint8_t *k_exp, *v_exp;   /* dev [num_blocks, Hkv, block_size, D / 32]; NULL for LA_BF16         */
+  void *k_bounds;           /* dev [num_blocks, Hkv, 2, D] bf16, smallest then largest, or NULL    */
+  int64_t exp_stride;       /* of further layers, in bytes (multiple of 16) and in elements         */
+  int64_t bounds_stride;    /* (multiple of 8); cache_stride of la_layer_strides is in elements     */
+} la_block_cache;
+
+LA_API la_status la_kv_store(
+    const la_attn_desc *desc,
+    const la_block_cache *cache,     /* host; rows, exponents and bounds are written                */
+    const int32_t *block_tables,     /* dev [B, max_blocks_per_request] or NULL (identity)          */
+    const int32_t *prefix_lens,      /* dev [B]                                                     */
+    const int32_t *prefix_lens_host, /* host [B], same values (room for prefix_lens_host[b] +
+                                        chain_len + branch_len positions is required)               */
+    const void *k_branch,            /* dev [B, gamma, L, Hkv, D] bf16 per layer                    */
+    const void *v_branch,
+    const void *k_chain,             /* dev [B, chain_len, Hkv, D] bf16 per layer; NULL if chain_len 0 */
+    const void *v_chain,
+    int32_t chain_len,
+    const int32_t *src_branch,       /* dev [B], or NULL = 0   (all three are clamped to their      */
+    const int32_t *n_chain,          /* dev [B], or NULL = 0    ranges, as in la_kv_commit)         */
+    const int32_t *n_own,            /* dev [B], or NULL = branch_len                               */
+    int32_t *new_prefix_lens,        /* dev [B], written; not prefix_lens                           */
+    const la_layer_strides *layers,  /* host, or NULL = one layer; scale_stride is not used         */
+    void *hip_stream);
+
+/* Rows first[b] .. first[b] + num_tokens - 1 of every request, as far as they
+ * lie in 0 .. prefix_lens[b] - 1, into row 0 .. of the outputs; the other rows
+ * of the outputs are left as they were.  desc->out_dtype: LA_BF16 (exact) or
+ * LA_F32.  layers: cache_stride as above, branch_stride the outputs' stride. */
+LA_API la_status la_kv_load(
+    const la_attn_desc *desc, const la_block_cache *cache, const int32_t *block_tables,
+    const int32_t *prefix_lens,      /* dev [B], clamped to what the block table maps               */
+    const int32_t *first,            /* dev [B], or NULL = 0                                        */
+    int32_t num_tokens,              /* >= 1                                                        */
+    void *k_out,                     /* dev [B, num_tokens, Hkv, D] out_dtype per layer             */
+    void *v_out,
+    const la_layer_strides *layers, void *hip_stream);
+
+/* Query tokens are taken in groups of group_len tokens of one branch (the last
+ * group of a branch may be shorter): num_groups = ceil(L / group_len) per
+ * branch.  For a group and KV head a block with bounds lo, hi scores
+ *     max over the group's rows q (tokens x query heads of the KV head) of
+ *     sum_d q_d * (q_d > 0 ? hi_d : lo_d),
+ * which no q . k of the block exceeds.  Of the request's
+ * ceil(prefix_lens / block_size) blocks max_blocks are listed (all, if there
+ * are no more): the first keep_first, the last keep_last, and of the others
+ * those with the largest scores, equal ones in the order of their index.  The
+ * order is that of the exact scores (fp64 where rounded ones do not settle it),
+ * not of rounded ones. */
+typedef struct {
+  int32_t group_len;      /* 1..branch_len                                     */
+  int32_t max_blocks;     /* >= 1                                              */
+  int32_t keep_first;     /* >= 0; keep_first + keep_last <= max_blocks        */
+  int32_t keep_last;
+} la_select_desc;
+
+LA_API la_status la_block_select_workspace(const la_attn_desc *desc, const la_select_desc *sel,
+                                           const int32_t *prefix_lens_host, size_t *bytes_out);
+LA_API la_status la_block_select(
+    const la_attn_desc *desc, const la_select_desc *sel,
+    const void *q,                   /* dev [B, gamma, L, Hq, D] bf16                               */
+    const void *k_bounds,            /* dev [num_blocks, Hkv, 2, D] bf16 of the layer               */
+    const int32_t *block_tables, const int32_t *prefix_lens, const int32_t *prefix_lens_host,
+    int32_t *blocks,                 /* dev [B, gamma, num_groups, Hkv, max_blocks] out: logical
+                                        blocks in ascending order, -1 behind the last               */
+    int32_t *counts,                 /* dev [B, gamma, num_groups, Hkv] out                         */
+    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* la_verify_attention over the listed blocks of a block cache instead of the
+ * whole prefix: every row attends to the keys of its group's list and to its
+ * branch's own tokens up to its own.  The lists hold distinct logical blocks in
+ * ascending order (la_block_select's, or the caller's own); counts outside
+ * 0..max_blocks and ids outside the prefix are clamped.  blocks == NULL (then
+ * sel and counts are NULL too): every block of the prefix.  Probabilities are
+ * rounded to bf16 before they meet V, as on la_verify_attention's MFMA path;
+ * lse is fp32-accurate.  out_dtype LA_BF16 or LA_F32. */
+LA_API la_status la_verify_attention_sparse_workspace(const la_attn_desc *desc, const la_select_desc *sel,
+                                                      const int32_t *prefix_lens_host, size_t *bytes_out);
+LA_API la_status la_verify_attention_sparse(
+    const la_attn_desc *desc, const la_select_desc *sel,
+    const void *q,                   /* dev [B, gamma, L, Hq, D] bf16                               */
+    const la_block_cache *cache,     /* host; k_bounds is not read                                  */
+    const int32_t *block_tables, const int32_t *prefix_lens, const int32_t *prefix_lens_host,
+    const int32_t *blocks,           /* dev [B, gamma, num_groups, Hkv, max_blocks], or NULL        */
+    const int32_t *counts,           /* dev [B, gamma, num_groups, Hkv], or NULL                    */
+    const void *k_branch,            /* dev [B, gamma, L, Hkv, D] bf16                              */
+    const void *v_branch,
+    void *out,                       /* dev [B, gamma, L, Hq, D]                                    */
+    float *lse,                      /* dev [B, gamma, L, Hq], or NULL                              */
+    void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* ------------------------------------------------------------------------- *
  *  la_spec_accept

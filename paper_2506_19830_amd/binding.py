@@ -20,8 +20,10 @@ _HERE = Path(__file__).resolve().parent
 LIB_PATH = _HERE / "libla_verify.so"
 BENCH_LIB_PATH = _HERE / "libla_verify_bench.so"
 
-LA_F32, LA_BF16, LA_FP8_E4M3 = 0, 1, 2
-DTYPE_CODES = {"f32": LA_F32, "bf16": LA_BF16, "fp8_e4m3": LA_FP8_E4M3}
+LA_F32, LA_BF16, LA_FP8_E4M3, LA_MXFP8_E4M3, LA_MXFP4_E2M1 = 0, 1, 2, 3, 4
+# (the mx formats: rows of a block cache only)
+DTYPE_CODES = {"f32": LA_F32, "bf16": LA_BF16, "fp8_e4m3": LA_FP8_E4M3, "mxfp8_e4m3": LA_MXFP8_E4M3,
+               "mxfp4_e2m1": LA_MXFP4_E2M1}
 _TORCH_DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8_e4m3": torch.float8_e4m3fn}
 
 EXPORTED_SYMBOLS = (
@@ -29,6 +31,8 @@ EXPORTED_SYMBOLS = (
     "la_verify_attention_tree", "la_kv_commit", "la_kv_commit_tree", "la_step_select_tree", "la_step_select",
     "la_speedup_step_sync", "la_speedup_step_async", "la_speedup_token", "la_plan_budget",
     "la_spec_accept_workspace", "la_spec_accept", "la_spec_accept_static", "la_status_string",
+    "la_kv_store", "la_kv_load", "la_block_select_workspace", "la_block_select", "la_verify_attention_sparse_workspace",
+    "la_verify_attention_sparse",
 )
 # what libla_verify_bench.so exports on top of those (la_verify_bench.h)
 BENCH_SYMBOLS = (
@@ -60,6 +64,15 @@ class la_accept_desc(ctypes.Structure):
 class la_layer_strides(ctypes.Structure):
     _fields_ = [("num_layers", ctypes.c_int32), ("cache_stride", ctypes.c_int64), ("branch_stride", ctypes.c_int64),
                 ("chain_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64)]
+
+
+class la_block_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_exp", "v_exp", "k_bounds")] + [
+        ("exp_stride", ctypes.c_int64), ("bounds_stride", ctypes.c_int64)]
+
+
+class la_select_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("group_len", "max_blocks", "keep_first", "keep_last")]
 
 
 class la_plan_desc(ctypes.Structure):
@@ -143,6 +156,22 @@ def load(kind: Optional[str] = None) -> ctypes.CDLL:
                                        ctypes.c_size_t, vp]
         lib.la_spec_accept_static.restype = ctypes.c_int
         lib.la_spec_accept_static.argtypes = [ctypes.POINTER(la_accept_desc)] + [vp] * 9
+        desc_p, cache_p, sel_p = (ctypes.POINTER(t) for t in (la_attn_desc, la_block_cache, la_select_desc))
+        lens_p, bytes_p = ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_size_t)
+        lib.la_kv_store.restype = ctypes.c_int
+        lib.la_kv_store.argtypes = [desc_p, cache_p, i32p, i32p, lens_p, vp, vp, vp, vp, ctypes.c_int32, i32p, i32p,
+                                    i32p, i32p, ctypes.POINTER(la_layer_strides), vp]
+        lib.la_kv_load.restype = ctypes.c_int
+        lib.la_kv_load.argtypes = [desc_p, cache_p, i32p, i32p, i32p, ctypes.c_int32, vp, vp,
+                                   ctypes.POINTER(la_layer_strides), vp]
+        for fn in (lib.la_block_select_workspace, lib.la_verify_attention_sparse_workspace):
+            fn.restype = ctypes.c_int
+            fn.argtypes = [desc_p, sel_p, lens_p, bytes_p]
+        lib.la_block_select.restype = ctypes.c_int
+        lib.la_block_select.argtypes = [desc_p, sel_p, vp, vp, i32p, i32p, lens_p, i32p, i32p, vp, ctypes.c_size_t, vp]
+        lib.la_verify_attention_sparse.restype = ctypes.c_int
+        lib.la_verify_attention_sparse.argtypes = [desc_p, sel_p, vp, cache_p, i32p, i32p, lens_p, i32p, i32p, vp, vp,
+                                                   vp, vp, vp, ctypes.c_size_t, vp]
         lib.la_status_string.restype = ctypes.c_char_p
         lib.la_status_string.argtypes = [ctypes.c_int]
         if kind == "bench":
@@ -322,6 +351,101 @@ def la_kv_commit_tree(desc: la_attn_desc, k_cache, v_cache, block_tables, prefix
                                   ctypes.byref(layers) if layers is not None else None, _stream())
     if st:
         raise LaError(st, "la_kv_commit_tree")
+
+
+# ------------------------------------------------------------------------------------------- block cache
+
+def make_block_cache(k, v, k_exp=None, v_exp=None, k_bounds=None) -> la_block_cache:
+    """The tensors of a block cache: elements ``k`` / ``v`` [.., num_blocks, Hkv, block_size, D] (bfloat16,
+    float8_e4m3fn, or uint8 of half the width for fp4), exponents [.., num_blocks, Hkv, block_size, D / 32] (uint8,
+    quantised formats) and bounds [.., num_blocks, Hkv, 2, D] (bfloat16, optional), with a leading dimension of layers
+    or without.  The descriptor keeps the tensors alive."""
+    for t in (k, v, k_exp, v_exp, k_bounds):
+        if t is not None and not t.is_contiguous():
+            raise ValueError("the tensors of a block cache are contiguous")
+
+    def stride(t):
+        return t.stride(0) if t is not None and t.dim() == 5 else 0
+    addresses = [None if t is None else t.data_ptr() for t in (k, v, k_exp, v_exp, k_bounds)]
+    cache = la_block_cache(*addresses, stride(k_exp), stride(k_bounds))
+    cache.tensors = (k, v, k_exp, v_exp, k_bounds)
+    return cache
+
+
+def make_select_desc(*, group_len, max_blocks, keep_first=0, keep_last=0) -> la_select_desc:
+    return la_select_desc(group_len, max_blocks, keep_first, keep_last)
+
+
+def _optional(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def la_kv_store(desc: la_attn_desc, cache: la_block_cache, block_tables, prefix_lens, prefix_lens_host, k_branch, v_branch,
+                k_chain, v_chain, src_branch, n_chain, n_own, new_prefix_lens,
+                layers: Optional[la_layer_strides] = None) -> None:
+    """Append tokens' K/V (bf16) to a block cache, quantised as ``desc`` says, and keep the bounds of its blocks.
+    ``k_chain`` / ``v_chain``, ``src_branch``, ``n_chain`` and ``n_own`` may be None (no chain, branch 0, nothing of the
+    chain, all of the branch)."""
+    C = 0 if k_chain is None else int(k_chain.shape[-3])
+    st = load().la_kv_store(ctypes.byref(desc), ctypes.byref(cache), _ptr(block_tables), _ptr(prefix_lens),
+                            _host_lens(prefix_lens_host), _ptr(k_branch), _ptr(v_branch), _ptr(k_chain), _ptr(v_chain), C,
+                            _ptr(src_branch), _ptr(n_chain), _ptr(n_own), _ptr(new_prefix_lens), _optional(layers),
+                            _stream())
+    if st:
+        raise LaError(st, "la_kv_store")
+
+
+def la_kv_load(desc: la_attn_desc, cache: la_block_cache, block_tables, prefix_lens, first, k_out, v_out,
+               layers: Optional[la_layer_strides] = None) -> None:
+    """Rows ``first[b]`` .. of every request into ``k_out`` / ``v_out`` [.., B, tokens, Hkv, D]; rows behind the prefix
+    are left as they were.  ``first`` may be None (from the start)."""
+    st = load().la_kv_load(ctypes.byref(desc), ctypes.byref(cache), _ptr(block_tables), _ptr(prefix_lens), _ptr(first),
+                           int(k_out.shape[-3]), _ptr(k_out), _ptr(v_out), _optional(layers), _stream())
+    if st:
+        raise LaError(st, "la_kv_load")
+
+
+def _sized(name: str, desc, sel, prefix_lens_host) -> int:
+    out = ctypes.c_size_t(0)
+    st = getattr(load(), name)(ctypes.byref(desc), _optional(sel), _host_lens(prefix_lens_host), ctypes.byref(out))
+    if st:
+        raise LaError(st, name)
+    return int(out.value)
+
+
+def la_block_select_workspace(desc: la_attn_desc, sel: la_select_desc, prefix_lens_host: Sequence[int]) -> int:
+    return _sized("la_block_select_workspace", desc, sel, prefix_lens_host)
+
+
+def la_block_select(desc: la_attn_desc, sel: la_select_desc, q, k_bounds, block_tables, prefix_lens, prefix_lens_host, blocks,
+                    counts, workspace) -> None:
+    """List the blocks of the prefix that matter most to every group of query tokens and KV head: ``blocks``
+    [B, gamma, groups, Hkv, max_blocks] (int32, ascending, -1 behind the last) and ``counts`` [B, gamma, groups, Hkv]."""
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = load().la_block_select(ctypes.byref(desc), _optional(sel), _ptr(q), _ptr(k_bounds), _ptr(block_tables),
+                                _ptr(prefix_lens), _host_lens(prefix_lens_host), _ptr(blocks), _ptr(counts),
+                                _ptr(workspace), ws_bytes, _stream())
+    if st:
+        raise LaError(st, "la_block_select")
+
+
+def la_verify_attention_sparse_workspace(desc: la_attn_desc, sel: Optional[la_select_desc],
+                                         prefix_lens_host: Sequence[int]) -> int:
+    return _sized("la_verify_attention_sparse_workspace", desc, sel, prefix_lens_host)
+
+
+def la_verify_attention_sparse(desc: la_attn_desc, sel: Optional[la_select_desc], q, cache: la_block_cache, block_tables,
+                               prefix_lens, prefix_lens_host, blocks, counts, k_branch, v_branch, out, lse,
+                               workspace) -> None:
+    """Verification attention over the listed blocks of a block cache and the branches' own tokens; ``sel``, ``blocks``
+    and ``counts`` None: over the whole prefix."""
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = load().la_verify_attention_sparse(ctypes.byref(desc), _optional(sel), _ptr(q), ctypes.byref(cache),
+                                           _ptr(block_tables), _ptr(prefix_lens), _host_lens(prefix_lens_host),
+                                           _ptr(blocks), _ptr(counts), _ptr(k_branch), _ptr(v_branch), _ptr(out), _ptr(lse),
+                                           _ptr(workspace), ws_bytes, _stream())
+    if st:
+        raise LaError(st, "la_verify_attention_sparse")
 
 
 def la_calibrate_mfma(workgroups: int, iters: int, sink, data: bool = False) -> float:

@@ -19,7 +19,8 @@ OBJ = HERE / "_build"
 LIB = HERE / "libla_verify.so"
 
 SOURCES = ["api.hip", "attn_mfma.hip", "attn_stream.hip", "attn_merge.hip", "attn_f32.hip", "attn_rows.hip",
-           "accept.hip", "accept_static.hip", "kv_commit.hip", "controller.hip"]
+           "accept.hip", "accept_static.hip", "kv_commit.hip", "controller.hip", "block_api.hip", "block_cache.hip",
+           "block_select.hip", "attn_blocks.hip"]
 # benchmark aids (per-kernel event timing, calibration kernels, a self-test hook): only in libla_verify_bench.so,
 # which is the product library's objects linked together with these
 BENCH_SOURCES = ["bench_aids.hip", "calibrate.hip"]
@@ -77,7 +78,7 @@ def build(verbose: bool = False, extra_flags=(), lib: Path = LIB, bench_lib: Pat
 # la_spec_accept_static.  build_host_sanitized() recompiles these with the host sanitizers (device code is compiled
 # as always) and links them with the other, unchanged objects into a library for the CPU test that exercises
 # every host path under AddressSanitizer and UndefinedBehaviorSanitizer.
-HOST_SOURCES = ["api.hip", "controller.hip", "accept_static.hip"]
+HOST_SOURCES = ["api.hip", "controller.hip", "accept_static.hip", "block_api.hip"]
 
 
 def asan_runtime() -> Path:

@@ -9,7 +9,6 @@
 #include <cstdio>
 
 namespace la {
-namespace {
 
 // Compute units of the current device, asked once (256 on MI355X, also the fallback when no device answers, e.g. a
 // workspace query on a machine without a GPU).
@@ -24,6 +23,8 @@ int num_cus() {
   });
   return cus;
 }
+
+namespace {
 
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }

@@ -11,7 +11,8 @@ namespace {
 
 const char *kSlotNames[SLOT_COUNT] = {"attn_mfma",     "attn_merge",   "attn_f32",   "accept_stats", "accept_warp",
                                       "accept_sample", "accept_pick", "kv_commit",
-                                      "calib_mfma",    "calib_read"};
+                                      "calib_mfma",    "calib_read",  "kv_store",   "kv_load",     "block_score",
+                                      "block_pick",    "attn_blocks"};
 struct ProfileRecord {
   int slot;
   hipEvent_t start, stop;

@@ -104,6 +104,11 @@ enum KernelSlot {
   SLOT_KV_COMMIT,
   SLOT_CALIB_MFMA,
   SLOT_CALIB_READ,
+  SLOT_KV_STORE,
+  SLOT_KV_LOAD,
+  SLOT_BLOCK_SCORE,
+  SLOT_BLOCK_PICK,
+  SLOT_ATTN_BLOCKS,
   SLOT_COUNT
 };
 
@@ -192,6 +197,73 @@ struct CommitParams {
 };
 // src_bytes: storage size of a source element; quantise: bf16 source into an fp8 cache
 hipError_t launch_kv_commit(const CommitParams &p, int src_bytes, bool quantise, hipStream_t stream);
+
+// ----------------------------------------------------------------------------
+// Block cache: rows kept in bf16 or quantised in groups of 32 elements, with the bounds of every block's keys.
+// ----------------------------------------------------------------------------
+int num_cus();  // compute units of the current device (256 when none answers)
+
+enum BlockFormat { FMT_BF16 = 0, FMT_MX8, FMT_MX4, FMT_COUNT };
+constexpr int kGroup = 32;                       // elements that share an exponent
+constexpr int kExpMin = -100, kExpMax = 100;     // range of the exponents; stored as exponent + kExpBias
+constexpr int kExpBias = 127;
+
+struct BlockStoreParams {
+  CommitParams c;          // caches, sources, decisions (k_scale, v_scale, pool_seg, commit_mask unused)
+  uint8_t *k_exp, *v_exp;  // [layers][num_blocks, Hkv, block_size, D / 32] (null: bf16)
+  void *k_bounds;          // [layers][num_blocks, Hkv, 2, D] bf16, or null
+  int64_t exp_stride, bounds_stride;
+  int n_dst;               // blocks that one request's new rows can touch
+};
+hipError_t launch_kv_store(const BlockStoreParams &p, int format, hipStream_t stream);
+
+struct BlockLoadParams {
+  const void *k_cache, *v_cache;
+  const uint8_t *k_exp, *v_exp;
+  const int32_t *block_tables, *prefix_lens, *first;
+  void *k_out, *v_out;     // [layers][B, T, Hkv, D]
+  int B, Hkv, D, T, block_shift, max_blocks, capacity, num_layers, out_f32;
+  int64_t cache_stride, exp_stride, out_stride;  // elements between consecutive layers
+};
+hipError_t launch_kv_load(const BlockLoadParams &p, int format, hipStream_t stream);
+
+// Block selection.  A group is group_len consecutive tokens of one branch (the last one of a branch may be shorter)
+// with the G query heads of a KV head; groups are numbered (b, g, index in the branch).
+struct SelectParams {
+  const void *q;              // [B, gamma, L, Hq, D] bf16
+  const void *k_bounds;       // [num_blocks, Hkv, 2, D] bf16
+  const int32_t *block_tables, *prefix_lens;
+  int32_t *blocks, *count;    // [B, gamma, groups, Hkv, max_sel], [B, gamma, groups, Hkv]
+  float *score;               // workspace [B * gamma * groups * Hkv, n_max]: rounded scores
+  float *top;                 // workspace [B * Hkv, n_tiles]: largest magnitude of 32 blocks' bounds
+  double *exact;              // workspace [B * gamma * groups * Hkv, n_max]: scores in fp64 where a decision needs them
+  int B, Hq, Hkv, G, D, gamma, L, group_len, n_groups, block_shift, max_blocks;
+  int max_sel, keep_first, keep_last;
+  int n_max;                  // blocks of the longest prefix
+  int n_tiles;                // ceil(n_max / 32)
+};
+hipError_t launch_block_select(const SelectParams &p, hipStream_t stream);
+
+// Attention over selected blocks (sel == null: all blocks of the prefix).  A unit is one (request, group, KV head, tile of
+// the group's rows); without a selection one group holds the rows of all branches.  Its keys, the selected prefix rows and
+// then the branch-private tokens, are dealt out in tiles of 32 over n_split workgroups.
+struct SparseParams {
+  const void *q, *k_cache, *v_cache, *k_branch, *v_branch;
+  const uint8_t *k_exp, *v_exp;
+  const int32_t *block_tables, *prefix_lens, *sel, *sel_count;
+  float *part_o, *part_ml;    // [n_split][B * n_rows, D], [n_split][B * n_rows, 2]; null: n_split == 1
+  void *out;
+  float *lse;
+  int B, Hq, Hkv, G, D, gamma, L, block_shift, max_blocks;
+  int max_sel, group_len, n_groups;   // n_groups: groups of one request
+  int tile_rows, n_row_tiles;         // of one group
+  int n_rows;                         // gamma * L * Hq
+  int n_split, out_f32;
+  float scale_log2;
+};
+int attn_blocks_max_slots();                       // block ids a workgroup can hold
+int attn_blocks_tile_rows(int D, int rows);        // rows per unit for groups of `rows` rows
+hipError_t launch_attn_blocks(const SparseParams &p, int format, hipStream_t stream);
 
 // ----------------------------------------------------------------------------
 // Optional per-kernel event timing.  The two hooks are defined only in the benchmark build of the library
