@@ -48,104 +48,187 @@ __device__ __forceinline__ void split_signs(const u32x4 q, u32x4 &neg, u32x4 &po
   }
 }
 
-// A wavefront scores 32 blocks for one group: their bounds stay in registers as matrix operands while the group's rows pass,
-// 32 at a time; the largest of a block's row sums is then a maximum over registers.
-template <int D>
+// A wavefront keeps the bounds of 32 blocks (NB tiles of them) in registers as matrix operands while query rows pass, 32 at a
+// time.  Groups of at most SLOT rows share such a tile of rows: with rows 8 q .. 8 q + 7 in registers 4 q .. 4 q + 3 of the
+// result, the largest of a group's rows is a maximum over registers and the two halves of the wavefront.  Larger groups take
+// several tiles (SLOT = 32).
+template <int D, int SLOT, int NB>
 __global__ __launch_bounds__(256) void block_score_kernel(const SelectParams p) {
-  constexpr int T = D / 16;
+  constexpr int T = D / 16, kShare = 32 / SLOT, kRegs = SLOT / 2;  // groups of a row tile; registers of a group
   const int lane = threadIdx.x & 63, ln = lane & 31, h = lane >> 5;
-  const int tile = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int tile = (blockIdx.x * 4 + (threadIdx.x >> 6)) * NB;
   uint32_t id = blockIdx.y + blockIdx.z * 65535u;
-  if (id >= (uint32_t)(p.B * p.gamma * p.n_groups * p.Hkv)) return;
-  const size_t unit = id;
+  if (id >= (uint32_t)(p.B * p.score_chunks * p.Hkv)) return;
   const int hk = (int)(id % (uint32_t)p.Hkv);
   id /= (uint32_t)p.Hkv;
-  const int per_req = p.gamma * p.n_groups;
-  const int b = (int)(id / (uint32_t)per_req), group = (int)(id % (uint32_t)per_req);
+  const int chunk = (int)(id % (uint32_t)p.score_chunks), b = (int)(id / (uint32_t)p.score_chunks);
   const int n = prefix_blocks(p, b);
   if (n <= p.max_sel || tile * 32 >= n) return;  // all blocks are taken / no such blocks
-  const int lb = min(tile * 32 + ln, n - 1);
-  const int blk = p.block_tables ? p.block_tables[(size_t)b * p.max_blocks + lb] : b * p.max_blocks + lb;
-  const uint8_t *src = (const uint8_t *)p.k_bounds + ((size_t)blk * p.Hkv + hk) * 4 * D + h * 16;
-  u32x4 lo[T], hi[T];
+  u32x4 lo[NB][T], hi[NB][T];
 #pragma unroll
-  for (int t = 0; t < T; ++t) lo[t] = *(const u32x4 *)(src + t * 32), hi[t] = *(const u32x4 *)(src + 2 * D + t * 32);
+  for (int nb = 0; nb < NB; ++nb) {
+    const int lb = min((tile + nb) * 32 + ln, n - 1);
+    const int blk = p.block_tables ? p.block_tables[(size_t)b * p.max_blocks + lb] : b * p.max_blocks + lb;
+    const uint8_t *src = (const uint8_t *)p.k_bounds + ((size_t)blk * p.Hkv + hk) * 4 * D + h * 16;
+#pragma unroll
+    for (int t = 0; t < T; ++t) lo[nb][t] = *(const u32x4 *)(src + t * 32), hi[nb][t] = *(const u32x4 *)(src + 2 * D + t * 32);
+  }
+  const int per_req = p.gamma * p.n_groups;
+  const int first = (int)((int64_t)chunk * p.score_tiles / p.score_chunks) * kShare;
+  const int end = min((int)((int64_t)(chunk + 1) * p.score_tiles / p.score_chunks) * kShare, per_req);
 
-  const int g = group / p.n_groups, t0 = (group - g * p.n_groups) * p.group_len;
-  const int n_rows = min(p.group_len, p.L - t0) * p.G;
-  const size_t tok0 = ((size_t)b * p.gamma + g) * p.L + t0;
-  float best = -INFINITY;
-  for (int r0 = 0; r0 < n_rows; r0 += 32) {
-    const int r = min(r0 + ln, n_rows - 1);  // surplus rows repeat the last one
-    const uint8_t *qs = (const uint8_t *)p.q + ((tok0 + r / p.G) * p.Hq + hk * p.G + r % p.G) * D * 2 + h * 16;
-    f32x16 s;
+  // rows of a group, and the place of its row r
+  auto rows_of = [&](int group, int &n_rows) __attribute__((always_inline)) {
+    const int g = group / p.n_groups, t0 = (group - g * p.n_groups) * p.group_len;
+    n_rows = min(p.group_len, p.L - t0) * p.G;
+    return (const uint8_t *)p.q + ((((size_t)b * p.gamma + g) * p.L + t0) * p.Hq + hk * p.G) * D * 2 + h * 16;
+  };
+  auto place = [&](int r) __attribute__((always_inline)) { return ((size_t)(r / p.G) * p.Hq + r % p.G) * D * 2; };
+  auto tile_scores = [&](const uint8_t *qs, f32x16 (&s)[NB]) __attribute__((always_inline)) {
+    u32x4 q[T];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) s[j] = 0.f;
+    for (int t = 0; t < T; ++t) q[t] = *(const u32x4 *)(qs + t * 32);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[nb][j] = 0.f;
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       u32x4 neg, pos;
-      split_signs(*(const u32x4 *)(qs + t * 32), neg, pos);
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, neg), __builtin_bit_cast(bf16x8, lo[t]), s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, pos), __builtin_bit_cast(bf16x8, hi[t]), s, 0, 0, 0);
+      split_signs(q[t], neg, pos);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, neg), __builtin_bit_cast(bf16x8, lo[nb][t]), s[nb], 0, 0, 0);
+        s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, pos), __builtin_bit_cast(bf16x8, hi[nb][t]), s[nb], 0, 0, 0);
+      }
     }
+  };
+  auto store = [&](int group, int nb, float best) __attribute__((always_inline)) {
+    const int lb = (tile + nb) * 32 + ln;
+    if (h == 0 && lb < n) p.score[(((size_t)b * per_req + group) * p.Hkv + hk) * p.n_max + lb] = best;
+  };
+  if constexpr (SLOT == 32) {
+    for (int group = first; group < end; ++group) {
+      int n_rows;
+      const uint8_t *base = rows_of(group, n_rows);
+      float best[NB];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) best = fmaxf(best, s[j]);
-  }
-  best = xhalf_max(best);
-  if (h == 0 && tile * 32 + ln < n) p.score[unit * p.n_max + tile * 32 + ln] = best;
-  if (group == 0) {  // the largest magnitude among the tile's bounds, once per request and head
-    uint32_t top = 0;
+      for (int nb = 0; nb < NB; ++nb) best[nb] = -INFINITY;
+      for (int r0 = 0; r0 < n_rows; r0 += 32) {
+        f32x16 s[NB];
+        tile_scores(base + place(min(r0 + ln, n_rows - 1)), s);  // (surplus rows repeat the last one)
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        top = max(top, max(lo[t][i] << 16 & 0x7fffffffu, lo[t][i] & 0x7fff0000u));
-        top = max(top, max(hi[t][i] << 16 & 0x7fffffffu, hi[t][i] & 0x7fff0000u));
+          for (int j = 0; j < 16; ++j) best[nb] = fmaxf(best[nb], s[nb][j]);
       }
 #pragma unroll
+      for (int nb = 0; nb < NB; ++nb) store(group, nb, xhalf_max(best[nb]));
+    }
+  } else {
+    for (int group = first; group < end; group += kShare) {
+      int n_rows;
+      const uint8_t *base = rows_of(min(group + ln / SLOT, end - 1), n_rows);
+      f32x16 s[NB];
+      tile_scores(base + place(min(ln % SLOT, n_rows - 1)), s);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int q = 0; q < kShare; ++q) {
+          float best = s[nb][q * kRegs];
+#pragma unroll
+          for (int j = 1; j < kRegs; ++j) best = fmaxf(best, s[nb][q * kRegs + j]);
+          best = xhalf_max(best);
+          if (group + q < end) store(group + q, nb, best);
+        }
+    }
+  }
+  if (chunk == 0) {  // the largest magnitude among the tiles' bounds, once per request and head
+    uint32_t top = 0;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t a = lo[nb][t][i], z = hi[nb][t][i];
+          top = max(top, max(max(a << 16 & 0x7fffffffu, a & 0x7fff0000u), max(z << 16 & 0x7fffffffu, z & 0x7fff0000u)));
+        }
+#pragma unroll
     for (int off = 1; off < 64; off <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
-    if (lane == 0) p.top[((size_t)b * p.Hkv + hk) * p.n_tiles + tile] = __builtin_bit_cast(float, top);
+    if (lane == 0) p.top[((size_t)b * p.Hkv + hk) * p.n_tiles + tile / NB] = __builtin_bit_cast(float, top);
   }
 }
 
-// Rank n (1 = the largest) among the keys of items 0 .. count - 1 that `key_of` gives (0: not an item): the key, and how
-// many items above it there are.  Eight bits at a time; every thread of the workgroup calls it.
-template <typename Key, typename F>
-__device__ Key key_of_rank(int count, int n, F key_of, int *above, uint32_t (&hist)[256], uint32_t (&found)[2]) {
+constexpr int kListed = 1024;  // blocks in doubt that are held in LDS
+
+// LDS of a workgroup of NT threads that picks blocks.  The functions on it are called by all of its threads.
+template <int NT>
+struct Shared {
+  uint32_t hist[256];
+  uint32_t key_lo[NT / 64], key_hi[NT / 64];
+  float size_q[NT / 64], size_k[NT / 64];
+  uint32_t bin, bin_above, bin_count, n_list, n_doubt, n_sure;
+  uint32_t list[64];
+  int doubt[kListed];
+  unsigned long long doubt_key[kListed];
+  uint8_t doubt_taken[kListed];
+  int count[8 * (NT / 64)];
+};
+
+// The bin (counted from the top) of sh.hist in which item `rank` from the top lies: sh.bin, the items above it and in it.
+template <int NT>
+__device__ __forceinline__ void find_bin(Shared<NT> &sh, uint32_t rank) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t own = 0, incl = 0;
+  if (wave < 4) {
+    own = incl = sh.hist[255 - tid];
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const uint32_t up = (uint32_t)__shfl_up((int)incl, off);
+      if (lane >= off) incl += up;
+    }
+    if (lane == 63) sh.key_lo[wave] = incl;
+  }
+  __syncthreads();
+  if (wave < 4) {
+    for (int w = 0; w < wave; ++w) incl += sh.key_lo[w];
+    if (incl >= rank && incl - own < rank) sh.bin = 255 - tid, sh.bin_above = incl - own, sh.bin_count = own;
+  }
+  __syncthreads();
+}
+
+// Item `rank` from the top among the keys (0: not an item) that `for_each` visits, and how many items lie above it: eight
+// bits at a time, from any number of items.
+template <int NT, typename Key, typename F>
+__device__ Key key_of_rank(Shared<NT> &sh, uint32_t rank, F for_each, uint32_t *above) {
+  constexpr int kBits = (int)sizeof(Key) * 8;
   Key prefix = 0;
-  int left = n;
-  for (int shift = (int)sizeof(Key) * 8 - 8; shift >= 0; shift -= 8) {
-    hist[threadIdx.x] = 0;
+  uint32_t left = rank;
+  for (int shift = kBits - 8; shift >= 0; shift -= 8) {
+    if (threadIdx.x < 256) sh.hist[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.bin = sh.bin_above = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < count; i += 256) {
-      const Key k = key_of(i);
-      if (k != 0 && (shift + 8 >= (int)sizeof(Key) * 8 || (k >> (shift + 8)) == (prefix >> (shift + 8))))
-        atomicAdd(&hist[(uint32_t)(k >> shift) & 255u], 1u);
-    }
+    for_each([&](Key k) {
+      if (k != 0 && (shift + 8 >= kBits || (k >> (shift + 8)) == (prefix >> (shift + 8))))
+        atomicAdd(&sh.hist[(uint32_t)(k >> shift) & 255u], 1u);
+    });
     __syncthreads();
-    if (threadIdx.x == 0) {
-      uint32_t run = 0;
-      int d = 255;
-      for (; d > 0 && run + hist[d] < (uint32_t)left; --d) run += hist[d];
-      found[0] = (uint32_t)d, found[1] = run;
-    }
-    __syncthreads();
-    prefix |= (Key)found[0] << shift;
-    left -= (int)found[1];
+    find_bin(sh, left);
+    prefix |= (Key)sh.bin << shift;
+    left -= sh.bin_above;
     __syncthreads();
   }
-  *above = n - left;
+  *above = rank - left;
   return prefix;
 }
 
-constexpr int kListed = 1024;  // blocks in doubt that are evaluated at a time
-
-// One workgroup picks the blocks of one group and KV head from their scores.
-template <int D>
-__global__ __launch_bounds__(256) void block_pick_kernel(const SelectParams p) {
-  __shared__ uint32_t hist[256], found[2];
-  __shared__ float red[4];
-  __shared__ int list[kListed], n_list, wave_count[4][2];
+// One workgroup picks the blocks of one group and KV head from their scores.  Up to 8 NT candidates stay in registers (IN_REG).
+// Bound by the latency of a dozen dependent steps over a few hundred numbers.
+template <int D, int NT, bool IN_REG>
+__global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
+  constexpr int kItems = 8, kWaves = NT / 64;
+  __shared__ Shared<NT> sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t id = blockIdx.x;
   const size_t unit = id;
@@ -156,16 +239,38 @@ __global__ __launch_bounds__(256) void block_pick_kernel(const SelectParams p) {
   const int n = prefix_blocks(p, b);
   int32_t *out = p.blocks + unit * p.max_sel;
   if (n <= p.max_sel) {
-    for (int i = tid; i < p.max_sel; i += 256) out[i] = i < n ? i : -1;
+    for (int i = tid; i < p.max_sel; i += NT) out[i] = i < n ? i : -1;
     if (tid == 0) p.count[unit] = n;
     return;
   }
   const int c0 = p.keep_first, c1 = n - p.keep_last;           // candidates
   const int want = p.max_sel - p.keep_first - p.keep_last;     // fewer than there are
+  if (tid == 0) p.count[unit] = p.max_sel;
+  for (int i = tid; i < c0; i += NT) out[i] = i;
+  for (int i = tid; i < p.keep_last; i += NT) out[c0 + want + i] = c1 + i;
+  if (want == 0) return;
   const float *score = p.score + unit * p.n_max;
-  double *exact = p.exact + unit * p.n_max;
+  float item[kItems];
+  if constexpr (IN_REG) {
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int i = c0 + tid + k * NT;
+      item[k] = i < c1 ? score[i] : -INFINITY;
+    }
+  }
+  // f(place of the candidate, its score, its number among the thread's)
+  auto for_each = [&](auto f) __attribute__((always_inline)) {
+    if constexpr (IN_REG) {
+#pragma unroll
+      for (int k = 0; k < kItems; ++k)
+        if (c0 + tid + k * NT < c1) f(c0 + tid + k * NT, item[k], k);
+    } else {
+      for (int i = c0 + tid; i < c1; i += NT) f(i, score[i], 0);
+    }
+  };
 
-  // the largest sum of magnitudes of a row, the largest magnitude of a bound: the error of the scores
+  // the largest sum of magnitudes of a row and the largest magnitude of a bound give the error of the scores; the smallest and
+  // the largest key
   const int g = group / p.n_groups, t0 = (group - g * p.n_groups) * p.group_len;
   const int n_rows = min(p.group_len, p.L - t0) * p.G;
   const size_t tok0 = ((size_t)b * p.gamma + g) * p.L + t0;
@@ -174,7 +279,7 @@ __global__ __launch_bounds__(256) void block_pick_kernel(const SelectParams p) {
   };
   float size_q = 0.f, size_k = 0.f;
   constexpr int kPer = D / 8;  // lanes that share a row
-  for (int i0 = 0; i0 < n_rows * kPer; i0 += 256) {
+  for (int i0 = 0; i0 < n_rows * kPer; i0 += NT) {
     const int i = i0 + tid;
     float a = 0.f;
     if (i < n_rows * kPer) {
@@ -187,107 +292,199 @@ __global__ __launch_bounds__(256) void block_pick_kernel(const SelectParams p) {
     for (int off = 1; off < kPer; off <<= 1) a += __shfl_xor(a, off);
     size_q = fmaxf(size_q, a);
   }
-  for (int i = tid; i < (n + 31) / 32; i += 256) size_k = fmaxf(size_k, p.top[((size_t)b * p.Hkv + hk) * p.n_tiles + i]);
-  auto all_max = [&](float v) __attribute__((always_inline)) {
+  for (int i = tid; i * p.top_blocks < n; i += NT) size_k = fmaxf(size_k, p.top[((size_t)b * p.Hkv + hk) * p.n_tiles + i]);
+  uint32_t key_lo = 0xffffffffu, key_hi = 0;
+  for_each([&](int, float s, int) { key_lo = min(key_lo, order_key(s)), key_hi = max(key_hi, order_key(s)); });
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) v = fmaxf(v, __shfl_xor(v, off));
-    __syncthreads();
-    if (lane == 0) red[wave] = v;
-    __syncthreads();
-    return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  };
-  size_q = all_max(size_q), size_k = all_max(size_k);
+  for (int off = 1; off < 64; off <<= 1) {
+    size_q = fmaxf(size_q, __shfl_xor(size_q, off)), size_k = fmaxf(size_k, __shfl_xor(size_k, off));
+    key_lo = min(key_lo, (uint32_t)__shfl_xor((int)key_lo, off)), key_hi = max(key_hi, (uint32_t)__shfl_xor((int)key_hi, off));
+  }
+  if (lane == 0) sh.size_q[wave] = size_q, sh.size_k[wave] = size_k, sh.key_lo[wave] = key_lo, sh.key_hi[wave] = key_hi;
+  if (tid == 0) sh.n_list = sh.n_doubt = sh.n_sure = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    size_q = fmaxf(size_q, sh.size_q[w]), size_k = fmaxf(size_k, sh.size_k[w]);
+    key_lo = min(key_lo, sh.key_lo[w]), key_hi = max(key_hi, sh.key_hi[w]);
+  }
   const float err = kScoreError<D> * 1.01f * size_q * size_k + 1e-30f;
 
-  float sure = INFINITY, out_of = INFINITY;  // above: certainly taken; below: certainly not
-  int above = 0, need = 0, n_doubt = 0;
-  if (want > 0) {
-    int rank_above;
-    const uint32_t kt = key_of_rank<uint32_t>(
-        c1 - c0, want, [&](int i) { return order_key(score[c0 + i]); }, &rank_above, hist, found);
-    const float t = key_value(kt);
-    sure = t + 2.f * err, out_of = t - 2.f * err;
-    int mine_sure = 0, mine_doubt = 0;
-    for (int i = c0 + tid; i < c1; i += 256) {
-      const float s = score[i];
-      mine_sure += s > sure ? 1 : 0, mine_doubt += s >= out_of && !(s > sure) ? 1 : 0;
+  // t, the score of rank `want`: bins of equal width between the smallest and the largest key, then inside the bin it lies in,
+  // until a wavefront can hold that
+  uint32_t left = (uint32_t)want;
+  while (key_lo != key_hi) {
+    const int shift = max(0, 24 - (int)__builtin_clz(key_hi - key_lo));
+    __syncthreads();
+    if (tid < 256) sh.hist[tid] = 0;
+    if (tid == 0) sh.bin = sh.bin_above = sh.bin_count = 0;
+    __syncthreads();
+    for_each([&](int, float s, int) {
+      const uint32_t k = order_key(s);
+      if (k >= key_lo && k <= key_hi) atomicAdd(&sh.hist[(k - key_lo) >> shift], 1u);
+    });
+    __syncthreads();
+    find_bin(sh, left);
+    left -= sh.bin_above;
+    const uint32_t count = sh.bin_count;
+    key_lo += sh.bin << shift;
+    key_hi = min(key_hi, key_lo + ((1u << shift) - 1u));
+    if (key_lo == key_hi || count > 64) continue;
+    for_each([&](int, float s, int) {
+      const uint32_t k = order_key(s);
+      if (k >= key_lo && k <= key_hi) sh.list[atomicAdd(&sh.n_list, 1u) & 63u] = k;
+    });
+    __syncthreads();
+    const uint32_t mine = lane < (int)count ? sh.list[lane] : 0u;
+    uint32_t above = 0, same = 0;
+    for (uint32_t j = 0; j < count; ++j) {
+      const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)mine, (int)j);
+      above += k > mine ? 1u : 0u, same += k == mine ? 1u : 0u;
     }
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) mine_sure += __shfl_xor(mine_sure, off), mine_doubt += __shfl_xor(mine_doubt, off);
-    if (lane == 0) wave_count[wave][0] = mine_sure, wave_count[wave][1] = mine_doubt;
-    __syncthreads();
-    for (int w = 0; w < 4; ++w) above += wave_count[w][0], n_doubt += wave_count[w][1];
-    need = want - above;
-    __syncthreads();
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(lane < (int)count && above < left && left <= above + same);
+    key_lo = key_hi = (uint32_t)__builtin_amdgcn_readlane((int)mine, hit ? __builtin_ctzll(hit) : 0);
   }
+  const float t = key_value(key_lo);
+  const float sure = t + 2.f * err, out_of = t - 2.f * err;  // above: certainly taken; below: certainly not
   auto in_doubt = [&](float s) __attribute__((always_inline)) { return s >= out_of && !(s > sure); };
 
-  uint64_t exact_t = 0;
-  int ties = n_doubt;  // blocks at the threshold that are taken, the lowest indices first
-  if (n_doubt > need) {
-    // exact scores of the blocks in doubt
-    auto evaluate = [&](int count) __attribute__((always_inline)) {
-      const int part = lane & 7, r8 = lane >> 3;
-      for (int k = wave; k < count; k += 4) {
-        const int lb = list[k];
-        const int blk = p.block_tables ? p.block_tables[(size_t)b * p.max_blocks + lb] : b * p.max_blocks + lb;
-        const uint8_t *bs = (const uint8_t *)p.k_bounds + ((size_t)blk * p.Hkv + hk) * 4 * D;
-        double best = -INFINITY;
-        for (int r0 = 0; r0 < n_rows; r0 += 8) {
-          const uint8_t *qs = row_of(min(r0 + r8, n_rows - 1));
-          double sum = 0.0;
+  int slot[kItems];
+  for_each([&](int i, float s, int k) {
+    if (s > sure) {
+      atomicAdd(&sh.n_sure, 1u);
+    } else if (in_doubt(s)) {
+      const uint32_t at = atomicAdd(&sh.n_doubt, 1u);
+      if (at < kListed) sh.doubt[at] = i, sh.doubt_key[at] = 0;
+      if constexpr (IN_REG) slot[k] = (int)at;
+    }
+  });
+  __syncthreads();
+  const uint32_t n_doubt = sh.n_doubt, need = (uint32_t)want - sh.n_sure;
+  const bool listed = IN_REG && n_doubt <= kListed;
+
+  // One wavefront: exact score of block lb over rows r0 .. r0 + 7, eight lanes to a row.
+  auto exact_rows = [&](int lb, int r0) __attribute__((always_inline)) {
+    const int blk = p.block_tables ? p.block_tables[(size_t)b * p.max_blocks + lb] : b * p.max_blocks + lb;
+    const uint8_t *bs = (const uint8_t *)p.k_bounds + ((size_t)blk * p.Hkv + hk) * 4 * D;
+    const uint8_t *qs = row_of(min(r0 + (lane >> 3), n_rows - 1));
+    double sum = 0.0;
 #pragma unroll
-          for (int c = 0; c < D / 64; ++c) {
-            const int at = (c * 8 + part) * 16;
-            const u32x4 q = *(const u32x4 *)(qs + at), lo = *(const u32x4 *)(bs + at), hi = *(const u32x4 *)(bs + 2 * D + at);
+    for (int c = 0; c < D / 64; ++c) {
+      const int at = (c * 8 + (lane & 7)) * 16;
+      const u32x4 q = *(const u32x4 *)(qs + at), lo = *(const u32x4 *)(bs + at), hi = *(const u32x4 *)(bs + 2 * D + at);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const uint32_t a = (q[w] << 16) >> 31 ? lo[w] << 16 : hi[w] << 16;
-              const uint32_t z = q[w] >> 31 ? lo[w] & 0xffff0000u : hi[w] & 0xffff0000u;
-              sum += (double)__builtin_bit_cast(float, q[w] << 16) * (double)__builtin_bit_cast(float, a);
-              sum += (double)__builtin_bit_cast(float, q[w] & 0xffff0000u) * (double)__builtin_bit_cast(float, z);
-            }
-          }
-          sum += __shfl_xor(sum, 1), sum += __shfl_xor(sum, 2), sum += __shfl_xor(sum, 4);
-          best = fmax(best, sum);
-        }
-        best = fmax(best, __shfl_xor(best, 8)), best = fmax(best, __shfl_xor(best, 16)), best = fmax(best, __shfl_xor(best, 32));
-        if (lane == 0) exact[lb] = best;
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t a = (q[w] << 16) >> 31 ? lo[w] << 16 : hi[w] << 16;
+        const uint32_t z = q[w] >> 31 ? lo[w] & 0xffff0000u : hi[w] & 0xffff0000u;
+        sum += (double)__builtin_bit_cast(float, q[w] << 16) * (double)__builtin_bit_cast(float, a);
+        sum += (double)__builtin_bit_cast(float, q[w] & 0xffff0000u) * (double)__builtin_bit_cast(float, z);
       }
-    };
-    if (tid == 0) n_list = 0;
-    __syncthreads();
-    for (int i0 = c0; i0 < c1; i0 += 256) {
-      const int i = i0 + tid;
-      if (i < c1 && in_doubt(score[i])) list[atomicAdd(&n_list, 1)] = i;
-      __syncthreads();
-      const int count = n_list;
-      if (count > kListed - 256 || i0 + 256 >= c1) {
-        evaluate(count);
-        __syncthreads();
-        if (tid == 0) n_list = 0;
+    }
+    sum += __shfl_xor(sum, 1), sum += __shfl_xor(sum, 2), sum += __shfl_xor(sum, 4);
+    sum = fmax(sum, __shfl_xor(sum, 8)), sum = fmax(sum, __shfl_xor(sum, 16));
+    return fmax(sum, __shfl_xor(sum, 32));
+  };
+
+  if (listed) {
+    if (n_doubt > need) {
+      const int parts = (n_rows + 7) / 8;
+      for (int w = wave; w < (int)n_doubt * parts; w += kWaves) {
+        const int k = w / parts;
+        const double s = exact_rows(sh.doubt[k], (w - k * parts) * 8);
+        if (lane == 0) atomicMax(&sh.doubt_key[k], (unsigned long long)order_key64(s));
       }
       __syncthreads();
     }
-    int exact_above;
-    exact_t = key_of_rank<uint64_t>(
-        c1 - c0, need, [&](int i) { return in_doubt(score[c0 + i]) ? order_key64(exact[c0 + i]) : 0ull; }, &exact_above, hist,
-        found);
-    ties = need - exact_above;
+    for (int k = tid; k < (int)n_doubt; k += NT) {
+      uint32_t better = 0;
+      if (n_doubt > need) {
+        const unsigned long long mine = sh.doubt_key[k];
+        const int mine_i = sh.doubt[k];
+        for (uint32_t j = 0; j < n_doubt; ++j) {
+          const unsigned long long other = sh.doubt_key[j];
+          better += other > mine || (other == mine && sh.doubt[j] < mine_i) ? 1u : 0u;
+        }
+      }
+      sh.doubt_taken[k] = better < need ? 1 : 0;
+    }
+    __syncthreads();
+    // the list, in ascending order: how many each wavefront takes of each of its eight rows of candidates, then their places
+    uint32_t takes = 0;
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      bool take = false;
+      if (c0 + tid + k * NT < c1) take = item[k] > sure || (in_doubt(item[k]) && sh.doubt_taken[slot[k]]);
+      const uint64_t mask = __builtin_amdgcn_ballot_w64(take);
+      if (lane == 0) sh.count[k * kWaves + wave] = __popcll(mask);
+      takes |= (uint32_t)take << k;
+    }
+    __syncthreads();
+    constexpr int kCounts = kItems * kWaves, kPerLane = (kCounts + 63) / 64;
+    int own[kPerLane], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kPerLane; ++j) {
+      own[j] = lane * kPerLane + j < kCounts ? sh.count[lane * kPerLane + j] : 0;
+      sum += own[j];
+    }
+    int incl = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int up = __shfl_up(incl, off);
+      if (lane >= off) incl += up;
+    }
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int at = k * kWaves + wave, holder = at / kPerLane;  // of the counts of row k and this wavefront
+      int before = __builtin_amdgcn_readlane(incl - sum, holder);
+#pragma unroll
+      for (int j = 0; j + 1 < kPerLane; ++j)
+        if (j < at % kPerLane) before += __builtin_amdgcn_readlane(own[j], holder);
+      const bool take = (takes >> k) & 1;
+      const int place = before + __popcll(__builtin_amdgcn_ballot_w64(take) & ((1ull << lane) - 1));
+      if (take && place < want) out[c0 + place] = c0 + tid + k * NT;
+    }
+    return;
   }
 
-  // the list, in ascending order
-  int at = 0, tied = 0;
-  for (int i0 = 0; i0 < n; i0 += 256) {
+  // Any number of candidates and of blocks in doubt: exact scores and all decisions go through memory.
+  double *exact = p.exact + unit * p.n_max;
+  unsigned long long exact_t = 0;
+  uint32_t ties = n_doubt;  // blocks at the threshold that are taken, the lowest indices first
+  if (n_doubt > need) {
+    for (int i0 = c0; i0 < c1; i0 += NT) {
+      const int i = i0 + tid;
+      __syncthreads();
+      if (tid == 0) sh.n_doubt = 0;
+      __syncthreads();
+      if (i < c1 && in_doubt(score[i])) sh.doubt[atomicAdd(&sh.n_doubt, 1u) % kListed] = i;  // (at most NT <= kListed)
+      __syncthreads();
+      for (int k = wave; k < (int)sh.n_doubt; k += kWaves) {
+        double s = -INFINITY;
+        for (int r0 = 0; r0 < n_rows; r0 += 8) s = fmax(s, exact_rows(sh.doubt[k], r0));
+        if (lane == 0) exact[sh.doubt[k]] = s;
+      }
+    }
+    __syncthreads();
+    uint32_t exact_above;
+    exact_t = key_of_rank<NT, unsigned long long>(
+        sh, need,
+        [&](auto visit) {
+          for (int i = c0 + tid; i < c1; i += NT) visit(in_doubt(score[i]) ? (unsigned long long)order_key64(exact[i]) : 0ull);
+        },
+        &exact_above);
+    ties = need - exact_above;
+  }
+  int at = 0;
+  uint32_t tied = 0;
+  for (int i0 = c0; i0 < c1; i0 += NT) {
     const int i = i0 + tid;
-    bool take = i < n && (i < c0 || i >= c1), tie = false;
-    if (i >= c0 && i < c1 && want > 0) {
+    bool take = false, tie = false;
+    if (i < c1) {
       const float s = score[i];
-      if (s > sure) {
-        take = true;
-      } else if (in_doubt(s)) {
+      take = s > sure;
+      if (!take && in_doubt(s)) {
         if (n_doubt > need) {
-          const uint64_t k = order_key64(exact[i]);
+          const unsigned long long k = order_key64(exact[i]);
           take = k > exact_t, tie = k == exact_t;
         } else {
           take = true;
@@ -295,35 +492,61 @@ __global__ __launch_bounds__(256) void block_pick_kernel(const SelectParams p) {
       }
     }
     const uint64_t tie_mask = __builtin_amdgcn_ballot_w64(tie), below = (1ull << lane) - 1;
-    if (lane == 0) wave_count[wave][1] = __popcll(tie_mask);
     __syncthreads();
-    int rank = tied + __popcll(tie_mask & below);
-    for (int w = 0; w < 4; ++w) rank += w < wave ? wave_count[w][1] : 0, tied += wave_count[w][1];
+    if (lane == 0) sh.count[wave] = __popcll(tie_mask);
+    __syncthreads();
+    uint32_t rank = tied + (uint32_t)__popcll(tie_mask & below);
+    for (int w = 0; w < kWaves; ++w) rank += w < wave ? (uint32_t)sh.count[w] : 0u, tied += (uint32_t)sh.count[w];
     take |= tie && rank < ties;
     const uint64_t mask = __builtin_amdgcn_ballot_w64(take);
-    if (lane == 0) wave_count[wave][0] = __popcll(mask);
+    if (lane == 0) sh.count[kWaves + wave] = __popcll(mask);
     __syncthreads();
     int place = at + __popcll(mask & below);
-    for (int w = 0; w < 4; ++w) place += w < wave ? wave_count[w][0] : 0, at += wave_count[w][0];
-    if (take && place < p.max_sel) out[place] = i;
-    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) place += w < wave ? sh.count[kWaves + w] : 0, at += sh.count[kWaves + w];
+    if (take && place < want) out[c0 + place] = i;
   }
-  for (int i = at + tid; i < p.max_sel; i += 256) out[i] = -1;
-  if (tid == 0) p.count[unit] = min(at, p.max_sel);
+}
+
+template <int D, int SLOT, int NB>
+hipError_t launch_score(SelectParams &p, hipStream_t stream) {
+  ProfileScope scope(SLOT_BLOCK_SCORE, stream);
+  const int64_t groups = (int64_t)p.gamma * p.n_groups;
+  p.score_tiles = (int)((groups + 32 / SLOT - 1) / (32 / SLOT));
+  p.top_blocks = 32 * NB;
+  const int64_t tiles = (p.n_max + 32 * NB - 1) / (32 * NB), wgs = (tiles + 3) / 4;
+  // wavefronts that go through several groups read their blocks' bounds once: as many as fill the chip about four times over
+  // (2048 workgroups), the groups shared out among them
+  int64_t chunks = (2048 + wgs * p.B * p.Hkv - 1) / (wgs * p.B * p.Hkv);
+  chunks = chunks < p.score_tiles ? chunks : p.score_tiles;
+  p.score_chunks = (int)chunks;
+  const int64_t units = chunks * p.B * p.Hkv;
+  const dim3 grid((unsigned)wgs, (unsigned)(units < 65535 ? units : 65535), (unsigned)((units + 65534) / 65535));
+  hipLaunchKernelGGL((block_score_kernel<D, SLOT, NB>), grid, dim3(256), 0, stream, p);
+  return hipGetLastError();
 }
 
 template <int D>
-hipError_t launch(const SelectParams &p, hipStream_t stream) {
-  const int64_t units = (int64_t)p.B * p.gamma * p.n_groups * p.Hkv;
+hipError_t launch(SelectParams p, hipStream_t stream) {
+  const int rows = p.group_len * p.G;
   if (p.n_max > p.max_sel) {
-    ProfileScope scope(SLOT_BLOCK_SCORE, stream);
-    const dim3 grid((unsigned)((p.n_tiles + 3) / 4), (unsigned)(units < 65535 ? units : 65535), (unsigned)((units + 65534) / 65535));
-    hipLaunchKernelGGL((block_score_kernel<D>), grid, dim3(256), 0, stream, p);
-    const hipError_t e = hipGetLastError();
+    hipError_t e;
+    if (rows <= 8)
+      e = launch_score<D, 8, 1>(p, stream);
+    else if (rows <= 16)
+      e = launch_score<D, 16, 1>(p, stream);
+    else
+      e = launch_score<D, 32, D <= 128 ? 2 : 1>(p, stream);
     if (e != hipSuccess) return e;
   }
   ProfileScope scope(SLOT_BLOCK_PICK, stream);
-  hipLaunchKernelGGL((block_pick_kernel<D>), dim3((unsigned)units), dim3(256), 0, stream, p);
+  const dim3 grid((unsigned)((int64_t)p.B * p.gamma * p.n_groups * p.Hkv));
+  // sixteen wavefronts where one group's work can use them: more candidates than four hold, or exact scores over many rows
+  if (p.n_max > 8 * 1024)
+    hipLaunchKernelGGL((block_pick_kernel<D, 1024, false>), grid, dim3(1024), 0, stream, p);
+  else if (p.n_max > 8 * 256 || rows > 64)
+    hipLaunchKernelGGL((block_pick_kernel<D, 1024, true>), grid, dim3(1024), 0, stream, p);
+  else
+    hipLaunchKernelGGL((block_pick_kernel<D, 256, true>), grid, dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
