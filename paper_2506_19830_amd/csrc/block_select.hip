@@ -161,6 +161,7 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectParams p) 
 }
 
 constexpr int kListed = 1024;  // blocks in doubt that are held in LDS
+constexpr int kPairs = 1024;   // (block, row) pairs whose exact sums decide them
 
 // LDS of a workgroup of NT threads that picks blocks.  The functions on it are called by all of its threads.
 template <int NT>
@@ -173,6 +174,7 @@ struct Shared {
   int doubt[kListed];
   unsigned long long doubt_key[kListed];
   uint8_t doubt_taken[kListed];
+  uint32_t n_pairs, pair[kPairs];
   int count[8 * (NT / 64)];
 };
 
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
     key_lo = min(key_lo, (uint32_t)__shfl_xor((int)key_lo, off)), key_hi = max(key_hi, (uint32_t)__shfl_xor((int)key_hi, off));
   }
   if (lane == 0) sh.size_q[wave] = size_q, sh.size_k[wave] = size_k, sh.key_lo[wave] = key_lo, sh.key_hi[wave] = key_hi;
-  if (tid == 0) sh.n_list = sh.n_doubt = sh.n_sure = 0;
+  if (tid == 0) sh.n_list = sh.n_doubt = sh.n_sure = sh.n_pairs = 0;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
@@ -362,11 +364,13 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
   const uint32_t n_doubt = sh.n_doubt, need = (uint32_t)want - sh.n_sure;
   const bool listed = IN_REG && n_doubt <= kListed;
 
-  // One wavefront: exact score of block lb over rows r0 .. r0 + 7, eight lanes to a row.
-  auto exact_rows = [&](int lb, int r0) __attribute__((always_inline)) {
+  auto bounds_of = [&](int lb) __attribute__((always_inline)) {
     const int blk = p.block_tables ? p.block_tables[(size_t)b * p.max_blocks + lb] : b * p.max_blocks + lb;
-    const uint8_t *bs = (const uint8_t *)p.k_bounds + ((size_t)blk * p.Hkv + hk) * 4 * D;
-    const uint8_t *qs = row_of(min(r0 + (lane >> 3), n_rows - 1));
+    return (const uint8_t *)p.k_bounds + ((size_t)blk * p.Hkv + hk) * 4 * D;
+  };
+  // The exact sum of row r and block lb, eight lanes to a row.
+  auto exact_row = [&](int lb, int r) __attribute__((always_inline)) {
+    const uint8_t *bs = bounds_of(lb), *qs = row_of(r);
     double sum = 0.0;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
@@ -380,14 +384,59 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
         sum += (double)__builtin_bit_cast(float, q[w] & 0xffff0000u) * (double)__builtin_bit_cast(float, z);
       }
     }
-    sum += __shfl_xor(sum, 1), sum += __shfl_xor(sum, 2), sum += __shfl_xor(sum, 4);
-    sum = fmax(sum, __shfl_xor(sum, 8)), sum = fmax(sum, __shfl_xor(sum, 16));
-    return fmax(sum, __shfl_xor(sum, 32));
+    sum += __shfl_xor(sum, 1), sum += __shfl_xor(sum, 2);
+    return sum + __shfl_xor(sum, 4);
+  };
+  // One wavefront: the largest over rows r0 .. r0 + 7.
+  auto exact_rows = [&](int lb, int r0) __attribute__((always_inline)) {
+    double s = exact_row(lb, min(r0 + (lane >> 3), n_rows - 1));
+    s = fmax(s, __shfl_xor(s, 8)), s = fmax(s, __shfl_xor(s, 16));
+    return fmax(s, __shfl_xor(s, 32));
   };
 
   if (listed) {
+    bool all_rows = true;
+    if (n_doubt > need && n_rows > 8) {
+      // of a group's rows only those can hold a block's largest exact sum whose rounded sum is within 2 e of the largest
+      // rounded one: the sums of the blocks in doubt once more, 32 of them at a time, and the few rows listed
+      for (int k0 = 0; k0 < (int)n_doubt; k0 += 32) {
+        const int k = k0 + (lane & 31), h = lane >> 5, lb = sh.doubt[min(k, (int)n_doubt - 1)];
+        const uint8_t *bs = bounds_of(lb) + h * 16;
+        const float least = score[lb] - 2.f * err;
+        for (int r0 = wave * 32; r0 < n_rows; r0 += kWaves * 32) {
+          const uint8_t *qs = row_of(min(r0 + (lane & 31), n_rows - 1)) + h * 16;
+          f32x16 s;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[j] = 0.f;
+#pragma unroll
+          for (int t = 0; t < D / 16; ++t) {
+            u32x4 neg, pos;
+            split_signs(*(const u32x4 *)(qs + t * 32), neg, pos);
+            const bf16x8 lo = *(const bf16x8 *)(bs + t * 32), hi = *(const bf16x8 *)(bs + 2 * D + t * 32);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, neg), lo, s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, pos), hi, s, 0, 0, 0);
+          }
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int r = r0 + (j >> 2) * 8 + h * 4 + (j & 3);
+            if (k < (int)n_doubt && r < n_rows && s[j] >= least) {
+              const uint32_t at = atomicAdd(&sh.n_pairs, 1u);
+              if (at < kPairs) sh.pair[at] = (uint32_t)r * kListed + (uint32_t)k;
+            }
+          }
+        }
+      }
+      __syncthreads();
+      const int n_pairs = (int)sh.n_pairs;
+      all_rows = n_pairs > kPairs;
+      for (int i0 = wave * 8; i0 < n_pairs && !all_rows; i0 += kWaves * 8) {
+        const uint32_t pair = sh.pair[min(i0 + (lane >> 3), n_pairs - 1)];
+        const double s = exact_row(sh.doubt[pair % kListed], (int)(pair / kListed));
+        if ((lane & 7) == 0) atomicMax(&sh.doubt_key[pair % kListed], (unsigned long long)order_key64(s));
+      }
+    }
     if (n_doubt > need) {
-      const int parts = (n_rows + 7) / 8;
+      const int parts = all_rows ? (n_rows + 7) / 8 : 0;
       for (int w = wave; w < (int)n_doubt * parts; w += kWaves) {
         const int k = w / parts;
         const double s = exact_rows(sh.doubt[k], (w - k * parts) * 8);
