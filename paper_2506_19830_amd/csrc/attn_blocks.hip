@@ -4,119 +4,285 @@
 // attend to the keys of these blocks and to the branch's own tokens up to their own:
 //     out = softmax(scale q.k) v   over both,   one pass with the running maximum and sum.
 //
-// A wavefront owns 32 (or 64) rows and walks over tiles of 32 keys on its own; the four wavefronts of a workgroup, and the
-// workgroups that share a unit, have disjoint tiles and are folded at the end.  The products are transposed:
-//     S^T (32 keys x 32 rows) = K Q^T,   O^T (D x 32 rows) += V^T P^T
+// The products are transposed,
+//     S^T (keys x rows) = K Q^T,   O^T (D x rows) += V^T P^T
 // so that a lane holds scores of one row only, and P^T leaves the accumulators of the first product in the order in which
-// the second one wants its operand (the keys of a tile are permuted alike on both sides).
-//   K goes from memory into matrix operands through registers alone: the lane of key n and half h holds the elements
-//     d = h D/2 .. of its row, 16 bytes per load, and the inner index of the product is permuted to match (Q likewise).
-//   V is widened to bf16 on its way into LDS (8 KB per wavefront at D = 128) and read back transposed by 16-bit reads.
-//   Quantised rows are widened exactly, with their exponents applied by the conversion.
+// the second one wants its operand (the keys of a tile are permuted alike on both sides).  V lies in LDS as bf16 and is read
+// back transposed by 16-bit reads.  Quantised rows are widened to bf16 exactly, their exponents applied by the conversion.
 // Probabilities are rounded to bf16 for the second product (relative 2^-9 each, of the size of the output's own rounding);
 // scores, maxima, sums and accumulators are fp32.
+//
+// Two kernels.  With up to 32 rows to a group (attn_rows_kernel) the work is a stream of keys that few rows look at: every
+// wavefront takes tiles of 32 keys of its own for all rows, K going from memory into matrix operands through registers
+// alone, and the wavefronts are folded at the end.  With more rows (attn_tile_kernel) four wavefronts of 32 rows each share
+// tiles of 64 keys that they widen into LDS together (up to 64 rows: two by two, each pair with half of a tile's keys).  Workgroups that share a group's keys leave partial results that the
+// merge of long splits joins.
 #include "attn_common.hpp"
 
 namespace la {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kMaxSlots = 2048;  // blocks whose place a workgroup holds in LDS
+constexpr int kMaxSlots = 1024;  // blocks whose place a workgroup holds in LDS
 
-// The half row of one key, as stored.
-template <int FMT, int D>
-struct Raw {
-  static constexpr int kWords = FMT == FMT_BF16 ? D / 4 : FMT == FMT_MX8 ? D / 8 : D / 16;
-  uint32_t w[kWords];
-  uint32_t e;  // exponents of the D / 64 groups, a byte each
-};
+typedef __attribute__((ext_vector_type(4))) short i16x4;
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
-template <int FMT, int D>
-__device__ __forceinline__ void load_half(Raw<FMT, D> &r, const void *base, const uint8_t *exps, size_t row, int h) {
-  const uint8_t *src = (const uint8_t *)base + (row * 2 + h) * (Raw<FMT, D>::kWords * 4);
-#pragma unroll
-  for (int i = 0; i < Raw<FMT, D>::kWords; i += 4) {
-    const u32x4 x = *(const u32x4 *)(src + i * 4);
-    r.w[i] = x[0], r.w[i + 1] = x[1], r.w[i + 2] = x[2], r.w[i + 3] = x[3];
-  }
-  if constexpr (FMT != FMT_BF16) {
-    const uint8_t *pe = exps + (row * 2 + h) * (D / 64);
-    if constexpr (D == 64)
-      r.e = *pe;
-    else if constexpr (D == 128)
-      r.e = *(const uint16_t *)pe;
-    else
-      r.e = *(const uint32_t *)pe;
-  }
-}
+__device__ __forceinline__ float exp_scale(uint32_t e) { return __builtin_bit_cast(float, e << 23); }
 
-// Elements 8 t .. 8 t + 7 of the half row as four bf16 pairs.
-template <int FMT, int D>
-__device__ __forceinline__ u32x4 widen(const Raw<FMT, D> &r, int t) {
+// Eight elements (bf16: four words, fp8: two, fp4: one) of scale s as four bf16 pairs.
+template <int FMT>
+__device__ __forceinline__ u32x4 widen8(const uint32_t *w, float s) {
   u32x4 x;
   if constexpr (FMT == FMT_BF16) {
-    x = u32x4{r.w[4 * t], r.w[4 * t + 1], r.w[4 * t + 2], r.w[4 * t + 3]};
+    x = u32x4{w[0], w[1], w[2], w[3]};
+  } else if constexpr (FMT == FMT_MX8) {
+    x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], s, false));
+    x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], s, true));
+    x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], s, false));
+    x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], s, true));
   } else {
-    const float s = __builtin_bit_cast(float, ((r.e >> (8 * (t / 4))) & 0xffu) << 23);
-    if constexpr (FMT == FMT_MX8) {
-      x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.w[2 * t], s, false));
-      x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.w[2 * t], s, true));
-      x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.w[2 * t + 1], s, false));
-      x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.w[2 * t + 1], s, true));
-    } else {
-      x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[t], s, 0));
-      x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[t], s, 1));
-      x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[t], s, 2));
-      x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[t], s, 3));
-    }
+    x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], s, 0));
+    x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], s, 1));
+    x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], s, 2));
+    x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], s, 3));
   }
   return x;
 }
+template <int FMT>
+constexpr int kWords8 = FMT == FMT_BF16 ? 4 : FMT == FMT_MX8 ? 2 : 1;
 
-// The 16-byte pieces of a V row lie permuted in LDS, piece c of key k at c ^ swizzle(k): the 16 keys that one store
-// instruction writes at a time, and the four keys x 64 bytes that one transposing read gathers, then fall into different
+// The 16-byte pieces of a row lie permuted in LDS, piece c of key k at c ^ swizzle(k): the 16 keys that a store or a read of
+// whole pieces touches at a time, and the keys x 32 or 64 bytes that one transposing read gathers, then fall evenly over the
 // banks.
 template <int D>
 __device__ __forceinline__ int swizzle(int key) {
   return D == 64 ? (((key >> 1) & 1) << 2) | ((key >> 2) & 3) : ((key & 3) << 2) | ((key >> 2) & 3);
 }
 
-typedef __attribute__((ext_vector_type(4))) short i16x4;
-typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+// Two transposing reads side by side: four keys of one element from each place.  (Joined as vectors of 16-bit numbers: joined
+// as 32-bit words, the compiler copied every pair of registers once more.)
+__device__ __forceinline__ bf16x8 read_transposed(const uint8_t *p0, const uint8_t *p1) {
+  const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)p0);
+  const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)p1);
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// 16 bytes per lane from memory to consecutive places in LDS, without registers in between; the wavefront that issues it waits
+// with wait_loads() before a barrier that lets others read.
+__device__ __forceinline__ void load_lds16(const uint8_t *src, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds_addr) : "m0");
+}
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }  // vmcnt(0)
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
+}
+
+// LDS written by some lanes is read by others of the same wavefront: the compiler must not move one across the other (the
+// hardware keeps a wavefront's LDS operations in order).
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Maximum / sum over the four lanes of a row (lane, lane ^ 16, lane ^ 32, lane ^ 48).
+__device__ __forceinline__ float quarter_max(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const auto sw = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t a = sw[0], b = sw[1];
+  return xhalf_max(fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+}
+__device__ __forceinline__ float quarter_sum(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const auto sw = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t a = sw[0], b = sw[1];
+  return xhalf_sum(__builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+}
+
+// What a workgroup works on.
+struct Unit {
+  int b, hk, tok0, n_rows, r0;  // request, KV head, first token of the group, its rows, the first one of this tile
+  int split;
+  int own0, own_end;            // own tokens that any row of the tile sees
+  int n_keys;                   // keys of the list
+  int begin, end, n_tiles;      // the workgroup's share of the unit's tiles; the first n_tiles of all are the list's
+  int slot0;                    // list index of place[0]
+};
+
+struct Places {
+  int32_t place[kMaxSlots];     // where the blocks lie that the workgroup's tiles come from
+  int32_t last;                 // the last block listed
+};
+
+// Finds the unit's rows and keys and fills the table of places (the caller's barrier makes it visible); false: no rows.  What
+// begins a workgroup is a chain of dependent loads, so everything that can be asked for at once is: a list that fits the table
+// is taken whole, without waiting for its length or the prefix's.
+template <int ROWS, int KEYS, int THREADS>
+__device__ __forceinline__ bool find_unit(const SparseParams &p, Unit &u, Places &t) {
+  // KV heads vary fastest: with eight of them each XCD keeps to one head's keys
+  uint32_t id = blockIdx.x;
+  u.hk = (int)(id % (uint32_t)p.Hkv);
+  id /= (uint32_t)p.Hkv;
+  u.split = (int)(id % (uint32_t)p.n_split);
+  id /= (uint32_t)p.n_split;
+  const int row_tile = (int)(id % (uint32_t)p.n_row_tiles);
+  id /= (uint32_t)p.n_row_tiles;
+  const int group = (int)(id % (uint32_t)p.n_groups);
+  u.b = (int)(id / (uint32_t)p.n_groups);
+  int n_tok = p.gamma * p.L;
+  u.tok0 = 0;
+  if (p.sel) {
+    const int per_branch = p.n_groups / p.gamma, g = group / per_branch, t0 = (group - g * per_branch) * p.group_len;
+    u.tok0 = g * p.L + t0;
+    n_tok = min(p.group_len, p.L - t0);
+  }
+  u.n_rows = n_tok * p.G, u.r0 = row_tile * ROWS;
+  if (u.r0 >= u.n_rows) return false;
+  const int r_last = min(u.r0 + ROWS, u.n_rows) - 1;
+  u.own0 = (u.tok0 + u.r0 / p.G) / p.L * p.L, u.own_end = u.tok0 + r_last / p.G + 1;
+
+  const int bs = 1 << p.block_shift, tid = threadIdx.x;
+  const int32_t *table = p.block_tables ? p.block_tables + (size_t)u.b * p.max_blocks : nullptr;
+  auto place_of = [&](int lb) __attribute__((always_inline)) { return table ? table[lb] : u.b * p.max_blocks + lb; };
+  const size_t unit = ((size_t)u.b * p.n_groups + group) * p.Hkv + u.hk;
+  const int32_t *list = p.sel ? p.sel + unit * p.max_sel : nullptr;
+  const bool whole = p.sel && p.max_sel <= kMaxSlots;
+  constexpr int kIds = (kMaxSlots + THREADS - 1) / THREADS;
+  int ids[kIds];
+  if (whole) {
+#pragma unroll
+    for (int k = 0; k < kIds; ++k)
+      if (tid + k * THREADS < p.max_sel) ids[k] = list[tid + k * THREADS];
+  }
+  const int listed = p.sel ? p.sel_count[unit] : 0;
+  const int P = (int)min((int64_t)max(p.prefix_lens[u.b], 0), (int64_t)p.max_blocks << p.block_shift);
+  const int n_blocks = (P + bs - 1) >> p.block_shift;
+  u.n_keys = P;
+  if (p.sel) {
+    const int n = min(max(listed, 0), min(p.max_sel, n_blocks));
+    int last = 0;
+    if (n > 0 && whole) {
+#pragma unroll
+      for (int k = 0; k < kIds; ++k) {
+        const int i = tid + k * THREADS, lb = min(max(ids[k], 0), n_blocks - 1);
+        if (i < n) t.place[i] = place_of(lb);
+        if (i == n - 1) t.last = lb;
+      }
+      __syncthreads();
+      last = t.last;
+    } else if (n > 0) {
+      last = min(max(list[n - 1], 0), n_blocks - 1);
+    }
+    u.n_keys = n > 0 ? ((n - 1) << p.block_shift) + min(bs, P - (last << p.block_shift)) : 0;
+  }
+  // the unit's tiles, dealt out evenly
+  u.n_tiles = (u.n_keys + KEYS - 1) / KEYS;
+  const uint32_t total = (uint32_t)(u.n_tiles + (u.own_end - u.own0 + KEYS - 1) / KEYS);
+  const uint32_t each = total / (uint32_t)p.n_split, more = total - each * (uint32_t)p.n_split;
+  u.begin = (int)(u.split * each + min((uint32_t)u.split, more));
+  u.end = u.begin + (int)(each + ((uint32_t)u.split < more ? 1u : 0u));
+  u.slot0 = 0;
+  if (!whole && u.begin < min(u.end, u.n_tiles)) {
+    u.slot0 = (u.begin * KEYS) >> p.block_shift;
+    const int slots = min(((min(u.end * KEYS, u.n_keys) - 1) >> p.block_shift) + 1 - u.slot0, kMaxSlots);
+    for (int i = tid; i < slots; i += THREADS)
+      t.place[i] = place_of(list ? min(max(list[u.slot0 + i], 0), n_blocks - 1) : u.slot0 + i);
+  }
+  return true;
+}
+
+__device__ __forceinline__ size_t out_row(const SparseParams &p, const Unit &u, int r) {
+  return (size_t)u.b * p.n_rows + (size_t)(u.tok0 + r / p.G) * p.Hq + u.hk * p.G + r % p.G;
+}
+
+// Four consecutive results of a row: the final values, or the workgroup's partial.
+__device__ __forceinline__ void put_out(const SparseParams &p, const Unit &u, size_t grow, int d, int D, f32x4 x, float inv) {
+  if (p.part_o) {
+    *(f32x4 *)(p.part_o + ((size_t)u.split * p.B * p.n_rows + grow) * D + d) = x;
+  } else if (p.out_f32) {
+    *(f32x4 *)((float *)p.out + grow * D + d) = x * inv;
+  } else {
+    x *= inv;
+    *(u32x2 *)((uint8_t *)p.out + (grow * D + d) * 2) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+  }
+}
+__device__ __forceinline__ void put_sums(const SparseParams &p, const Unit &u, size_t grow, float m, float l) {
+  if (p.part_o)
+    *(f32x2 *)(p.part_ml + ((size_t)u.split * p.B * p.n_rows + grow) * 2) = f32x2{m, l};
+  else if (p.lse)
+    p.lse[grow] = 0.69314718055994530942f * (m + __builtin_log2f(l));
+}
+
+enum TileMask { TILE_FULL = 0, TILE_TAIL, TILE_OWN };
+
+// ---------------------------------------------------------------------------------------------------- few rows
+
+// A quarter of one key's row, as stored: elements q D/4 .. of quarter q.
+template <int FMT, int D>
+struct Quarter {
+  static constexpr int kWords = D / 32 * kWords8<FMT>;
+  uint32_t w[kWords];
+  uint32_t e;  // the aligned word of exponents that holds those of its group (D = 256: of its two groups)
+};
+// (A word, and the byte taken out of it at its use: bytes were widened to registers right behind the loads, which waited for
+// memory in every tile.)
+template <int D>
+__device__ __forceinline__ int exp_shift(size_t row, int q) { return (int)((row * (D / 32) + q * D / 128) & 3) * 8; }
+
+template <int FMT, int D>
+__device__ __forceinline__ void load_quarter(Quarter<FMT, D> &r, const void *base, const uint8_t *exps, size_t row, int q) {
+  constexpr int N = Quarter<FMT, D>::kWords;
+  const uint8_t *src = (const uint8_t *)base + (row * 4 + q) * (N * 4);
+  if constexpr (N == 2) {
+    const u32x2 x = *(const u32x2 *)src;
+    r.w[0] = x[0], r.w[1] = x[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const u32x4 x = *(const u32x4 *)(src + i * 4);
+      r.w[i] = x[0], r.w[i + 1] = x[1], r.w[i + 2] = x[2], r.w[i + 3] = x[3];
+    }
+  }
+  if constexpr (FMT != FMT_BF16) r.e = *(const uint32_t *)(exps + ((row * (D / 32) + q * D / 128) & ~(size_t)3));
+}
+
+// shift: of the first group's exponent in its word
+template <int FMT, int D>
+__device__ __forceinline__ u32x4 widen(const Quarter<FMT, D> &r, int t, int shift) {
+  return widen8<FMT>(r.w + t * kWords8<FMT>, FMT == FMT_BF16 ? 0.f : exp_scale((r.e >> (shift + 8 * (t / 4))) & 0xffu));
+}
 
 template <int D, int RB>
 struct Rows {
-  bf16x8 q[RB][D / 16];
-  f32x16 o[RB][D / 32];
+  bf16x8 q[RB][D / 32];        // row n of block rb: elements quarter (D / 4) + 8 t ..
+  f32x4 o[RB][D / 16];         // O^T: row n, d = 16 db + 4 quarter + 0..3
   float m[RB], l[RB];          // running maximum (log2 units) and this lane's share of the sum
   int tok[RB], start[RB];      // token of the row inside the request, first token of its branch
 };
 
-enum TileMask { TILE_FULL = 0, TILE_TAIL, TILE_OWN };
-
-// Scores of one tile from the K half rows, then probabilities, then the product with the V tile in LDS.
-// first: index of the tile's first key; limit: keys from there on do not exist (TILE_TAIL).
+// Scores of the 32 keys of a tile, probabilities, and the product with the V tile in LDS.  first: the tile's first key; keys
+// from `limit` on do not exist (TILE_TAIL).
 template <int D, int RB, int MASK>
-__device__ __forceinline__ void attend(Rows<D, RB> &st, f32x16 (&s)[RB], const uint8_t *vt, float scale_log2, int first,
-                                       int limit, int lane) {
-  const int h = lane >> 5;
+__device__ __forceinline__ void attend_rows(Rows<D, RB> &st, f32x4 (&s)[RB][2], const uint8_t *lds, int vt_read, float scale_log2, int first,
+                                            int limit, int lane) {
+  const int quarter = lane >> 4;
   float alpha[RB];
   bool raise = false;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     float top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const int key = first + (j >> 2) * 8 + h * 4 + (j & 3);
-      s[rb][j] *= scale_log2;
-      if constexpr (MASK == TILE_TAIL) {
-        if (key >= limit) s[rb][j] = -INFINITY;
-      } else if constexpr (MASK == TILE_OWN) {
-        if (key > st.tok[rb] || key < st.start[rb]) s[rb][j] = -INFINITY;
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = first + 16 * u + 4 * quarter + j;
+        if constexpr (MASK == TILE_TAIL) {
+          if (key >= limit) s[rb][u][j] = -INFINITY;
+        } else if constexpr (MASK == TILE_OWN) {
+          if (key > st.tok[rb] || key < st.start[rb]) s[rb][u][j] = -INFINITY;
+        }
+        top = fmaxf(top, s[rb][u][j]);
       }
-      top = fmaxf(top, s[rb][j]);
-    }
-    top = xhalf_max(top);
+    top = quarter_max(top) * scale_log2;
     // the maximum is raised only when a tile exceeds it by kRaise: until then probabilities may reach 2^kRaise
     const bool up = top > st.m[rb] + kRaise;
     const float m = up ? top : st.m[rb];
@@ -129,211 +295,184 @@ __device__ __forceinline__ void attend(Rows<D, RB> &st, f32x16 (&s)[RB], const u
     for (int rb = 0; rb < RB; ++rb) {
       st.l[rb] *= alpha[rb];
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) st.o[rb][db][j] *= alpha[rb];
+      for (int db = 0; db < D / 16; ++db) st.o[rb][db] *= alpha[rb];
     }
   }
-  bf16x8 pf[RB][2];
+  // V^T operands: lane (d, quarter) takes keys 4 quarter + 0..3 and 16 more, the order of the probabilities.  A batch is read
+  // while the exponentials run, the next one while the matrix cores work on it.
+  constexpr int kBatch = 4;
+  bf16x8 vf[2][kBatch];
+  auto read_batch = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int db = 0; db < kBatch; ++db) {
+      const uint8_t *at = lds + (vt_read ^ ((i * kBatch + db) << 5));
+      vf[i & 1][db] = read_transposed(at, at + 16 * D * 2);
+    }
+  };
+  read_batch(0);
+  __builtin_amdgcn_sched_barrier(0);
+  bf16x8 pf[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const float base = st.m[rb] == -INFINITY ? 0.f : st.m[rb];  // no key seen yet: every score is -inf
     float sum = 0.f;
+    u32x4 w;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      u32x4 w;
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p0 = __builtin_amdgcn_exp2f(s[rb][8 * c + 2 * i] - base);
-        const float p1 = __builtin_amdgcn_exp2f(s[rb][8 * c + 2 * i + 1] - base);
+      for (int j = 0; j < 4; j += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][u][j], scale_log2, -base));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][u][j + 1], scale_log2, -base));
         sum += p0 + p1;
-        w[i] = pack_bf16(p0, p1);
+        w[2 * u + j / 2] = pack_bf16(p0, p1);
       }
-      pf[rb][c] = __builtin_bit_cast(bf16x8, w);
-    }
+    pf[rb] = __builtin_bit_cast(bf16x8, w);
     st.l[rb] += sum;
   }
-  // V^T operands: lane (d, h) takes keys 16 c + 4 h + 0..3 and + 8, the order of the probabilities above
-  const int i = lane & 15, sub = (lane >> 4) & 1;
 #pragma unroll
-  for (int c = 0; c < 2; ++c)
+  for (int i = 0; i < D / 16 / kBatch; ++i) {
+    if (i + 1 < D / 16 / kBatch) {
+      read_batch(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int key = 16 * c + 8 * e + 4 * h + (i >> 2);
-        const int piece = (4 * db + 2 * sub + ((i & 3) >> 1)) ^ swizzle<D>(key);
-        const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(vt + key * D * 2 + piece * 16 + (i & 1) * 8));
-        const u32x2 y = __builtin_bit_cast(u32x2, x);
-        w[2 * e] = y[0], w[2 * e + 1] = y[1];
-      }
-      const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
+    for (int db = 0; db < kBatch; ++db)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
-        st.o[rb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[rb][c], st.o[rb][db], 0, 0, 0);
-    }
+        st.o[rb][i * kBatch + db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i & 1][db], pf[rb], st.o[rb][i * kBatch + db], 0, 0, 0);
+  }
 }
 
+// (u: which 16 of the tile's 32 keys)
 template <int FMT, int D, int RB>
-__device__ __forceinline__ void scores(f32x16 (&s)[RB], const Raw<FMT, D> &k, const Rows<D, RB> &st) {
+__device__ __forceinline__ void scores_rows(f32x4 (&s)[RB][2], int u, const Quarter<FMT, D> &k, int shift, const Rows<D, RB> &st) {
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb)
+  for (int rb = 0; rb < RB; ++rb) s[rb][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 16; ++j) s[rb][j] = 0.f;
+  for (int t = 0; t < D / 32; ++t) {
+    const bf16x8 kf = __builtin_bit_cast(bf16x8, widen<FMT, D>(k, t, shift));
 #pragma unroll
-  for (int t = 0; t < D / 16; ++t) {
-    const bf16x8 kf = __builtin_bit_cast(bf16x8, widen<FMT, D>(k, t));
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) s[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, st.q[rb][t], s[rb], 0, 0, 0);
+    for (int rb = 0; rb < RB; ++rb) s[rb][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, st.q[rb][t], s[rb][u], 0, 0, 0);
   }
 }
 
 template <int FMT, int D>
-__device__ __forceinline__ void stage_v(uint8_t *vt, const Raw<FMT, D> &v, int key, int h) {
+__device__ __forceinline__ void stage_rows(uint8_t *lds, int vt_write, int u, const Quarter<FMT, D> &v, int shift) {
 #pragma unroll
-  for (int t = 0; t < D / 16; ++t) {
-    const int piece = (h * (D / 16) + t) ^ swizzle<D>(key);
-    *(u32x4 *)(vt + key * D * 2 + piece * 16) = widen<FMT, D>(v, t);
-  }
+  for (int t = 0; t < D / 32; ++t) *(u32x4 *)(lds + (vt_write ^ (t << 4)) + u * 16 * D * 2) = widen<FMT, D>(v, t, shift);
 }
 
-// LDS written by some lanes is read by others of the same wavefront: the compiler must not move one across the other (the
-// hardware keeps a wavefront's LDS operations in order).
-__device__ __forceinline__ void wave_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
+// Wavefronts of a SIMD that the registers are allotted for: a wavefront alone issues a vector instruction about every other
+// time it could, so as many as the accumulators leave room for.
 template <int FMT, int D, int RB>
-__global__ __launch_bounds__(256, RB == 1 && D <= 128 ? 2 : 1) void attn_blocks_kernel(const SparseParams p) {
-  constexpr int kTileBytes = 32 * D * 2;                 // V tile of a wavefront
-  constexpr int kFoldBytes = 2 * RB * (D / 32) * 16 * 64 * 4;  // accumulators of two wavefronts
-  constexpr int kBytes = kWaves * kTileBytes > kFoldBytes ? kWaves * kTileBytes : kFoldBytes;
+constexpr int kRowsOccupancy = D == 256 ? (RB == 1 ? 2 : 1) : RB == 2 ? 2 : D == 128 ? 3 : 4;
+
+template <int FMT, int D, int RB, int NW>
+__global__ __launch_bounds__(64 * NW, (kRowsOccupancy<FMT, D, RB>)) void attn_rows_kernel(const SparseParams p) {
+  constexpr int kTileBytes = 32 * D * 2;            // V tile of a wavefront
+  constexpr int kOne = RB * (D / 16) * 4 * 64;      // floats of one wavefront's accumulators
+  constexpr int kBytes = NW * kTileBytes > NW / 2 * kOne * 4 ? NW * kTileBytes : NW / 2 * kOne * 4;
   __shared__ __attribute__((aligned(16))) uint8_t lds[kBytes];
-  __shared__ int32_t place[kMaxSlots];
-  __shared__ float fold_ml[kWaves][RB * 32][2];
+  __shared__ Places places;
+  __shared__ float fold_ml[NW][RB * 16][2];
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ln = lane & 31, h = lane >> 5;
-  // KV heads vary fastest: with eight of them each XCD keeps to one head's keys
-  uint32_t id = blockIdx.x;
-  const int hk = (int)(id % (uint32_t)p.Hkv);
-  id /= (uint32_t)p.Hkv;
-  const int split = (int)(id % (uint32_t)p.n_split);
-  id /= (uint32_t)p.n_split;
-  const int row_tile = (int)(id % (uint32_t)p.n_row_tiles);
-  id /= (uint32_t)p.n_row_tiles;
-  const int group = (int)(id % (uint32_t)p.n_groups), b = (int)(id / (uint32_t)p.n_groups);
-
-  // rows of the unit
-  int tok0 = 0, n_tok = p.gamma * p.L;
-  if (p.sel) {
-    const int per_branch = p.n_groups / p.gamma, g = group / per_branch, t0 = (group - g * per_branch) * p.group_len;
-    tok0 = g * p.L + t0;
-    n_tok = min(p.group_len, p.L - t0);
-  }
-  const int n_group_rows = n_tok * p.G, r0 = row_tile * (RB * 32);
-  if (r0 >= n_group_rows) return;
-  const int r_last = min(r0 + RB * 32, n_group_rows) - 1;
-  const int own0 = (tok0 + r0 / p.G) / p.L * p.L, own_end = tok0 + r_last / p.G + 1;  // own tokens any row sees
-
-  // keys of the prefix
-  const int bs = 1 << p.block_shift;
-  const int P = (int)min((int64_t)max(p.prefix_lens[b], 0), (int64_t)p.max_blocks << p.block_shift);
-  const int n_blocks = (P + bs - 1) >> p.block_shift;
-  const size_t unit = ((size_t)b * p.n_groups + group) * p.Hkv + hk;
-  const int32_t *list = p.sel ? p.sel + unit * p.max_sel : nullptr;
-  int n_keys = P;
-  if (p.sel) {
-    const int n = min(max(p.sel_count[unit], 0), min(p.max_sel, n_blocks));
-    n_keys = 0;
-    if (n > 0) {
-      const int last = min(max(list[n - 1], 0), n_blocks - 1);
-      n_keys = ((n - 1) << p.block_shift) + min(bs, P - (last << p.block_shift));
-    }
-  }
-  const int n_tiles = (n_keys + 31) >> 5, n_own_tiles = (own_end - own0 + 31) >> 5;
-  const int64_t total = (int64_t)n_tiles + n_own_tiles, slots = (int64_t)p.n_split * kWaves;
-  const int s0 = split * kWaves;
-  const int wg_begin = (int)(s0 * total / slots), wg_end = (int)((s0 + kWaves) * total / slots);
-  const int begin = (int)((s0 + wave) * total / slots), end = (int)((s0 + wave + 1) * total / slots);
-
-  // where the blocks of the workgroup's tiles lie
-  const int slot0 = (wg_begin * 32) >> p.block_shift;
-  if (wg_begin < min(wg_end, n_tiles)) {
-    const int slot_end = ((min(wg_end * 32, n_keys) - 1) >> p.block_shift) + 1;
-    for (int i = threadIdx.x; i < slot_end - slot0; i += 256) {
-      const int lb = list ? min(max(list[slot0 + i], 0), n_blocks - 1) : slot0 + i;
-      const int blk = p.block_tables ? p.block_tables[(size_t)b * p.max_blocks + lb] : b * p.max_blocks + lb;
-      place[i] = blk;
-    }
-  }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, quarter = lane >> 4;
+  Unit u;
+  if (!find_unit<RB * 16, 32, 64 * NW>(p, u, places)) return;
+  const int n_tiles = u.n_tiles;
+  const int each = (u.end - u.begin) / NW, more = (u.end - u.begin) % NW;
+  const int begin = u.begin + wave * each + min(wave, more), end = begin + each + (wave < more ? 1 : 0);
 
   Rows<D, RB> st;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const int r = min(r0 + rb * 32 + ln, n_group_rows - 1);
-    const int tok = tok0 + r / p.G, head = hk * p.G + r % p.G;
-    const uint8_t *src = (const uint8_t *)p.q + (((size_t)b * p.gamma * p.L + tok) * p.Hq + head) * D * 2 + h * D;
+    const int r = min(u.r0 + rb * 16 + n, u.n_rows - 1);
+    const int tok = u.tok0 + r / p.G;
+    const uint8_t *src = (const uint8_t *)p.q + out_row(p, u, r) * D * 2 + quarter * (D / 2);
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) st.q[rb][t] = *(const bf16x8 *)(src + t * 16);
+    for (int t = 0; t < D / 32; ++t) st.q[rb][t] = *(const bf16x8 *)(src + t * 16);
     st.tok[rb] = tok, st.start[rb] = tok / p.L * p.L;
     st.m[rb] = -INFINITY, st.l[rb] = 0.f;
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) st.o[rb][db][j] = 0.f;
+    for (int db = 0; db < D / 16; ++db) st.o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   __syncthreads();
 
-  uint8_t *vt = lds + wave * kTileBytes;
+  // offsets into LDS (a row's pieces are permuted inside the row, whose size is a power of two: pieces are reached by XOR)
+  const int vt_write = wave * kTileBytes + n * D * 2 + (((quarter * (D / 32)) ^ swizzle<D>(n)) << 4);
+  const int read_key = 4 * quarter + (n >> 2);
+  const int vt_read = wave * kTileBytes + read_key * D * 2 + ((((n & 3) >> 1) ^ swizzle<D>(read_key)) << 4) + (n & 1) * 8;
   // the prefix: the rows of the next tile are requested before the present one is used
   const int pre_end = min(end, n_tiles);
   if (begin < pre_end) {
-    auto row_of = [&](int tile) __attribute__((always_inline)) {
-      const int key = min(tile * 32 + ln, n_keys - 1);
-      const int blk = place[(key >> p.block_shift) - slot0];
-      return ((((size_t)blk * p.Hkv + hk) << p.block_shift) + (key & (bs - 1)));
+    auto row_of = [&](int tile, int x) __attribute__((always_inline)) {
+      const int key = min(tile * 32 + x * 16 + n, u.n_keys - 1);
+      const int blk = places.place[(key >> p.block_shift) - u.slot0];
+      return (((size_t)blk * p.Hkv + u.hk) << p.block_shift) + (key & ((1 << p.block_shift) - 1));
     };
-    Raw<FMT, D> k, v;
-    size_t row = row_of(begin);
-    load_half(k, p.k_cache, p.k_exp, row, h);
-    load_half(v, p.v_cache, p.v_exp, row, h);
-    for (int tile = begin; tile < pre_end; ++tile) {
-      const size_t next = row_of(min(tile + 1, pre_end - 1));
-      stage_v(vt, v, ln, h);
-      load_half(v, p.v_cache, p.v_exp, next, h);
-      f32x16 s[RB];
-      scores(s, k, st);
-      load_half(k, p.k_cache, p.k_exp, next, h);
+    // A tile's registers are requested anew as soon as its scores and its V tile are made; the scheduling fence keeps the
+    // compiler from moving the requests down to where the next tile needs them.
+    Quarter<FMT, D> k[2], v[2];
+    auto request = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const size_t row = row_of(min(tile, pre_end - 1), x);
+        load_quarter(v[x], p.v_cache, p.v_exp, row, quarter);
+        load_quarter(k[x], p.k_cache, p.k_exp, row, quarter);
+      }
+    };
+    // (a block's rows begin at a multiple of 16, so the key says where in its word an exponent is)
+    auto consume = [&](f32x4 (&s)[RB][2], int last) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int shift = exp_shift<D>((size_t)min(x * 16 + n, last), quarter);
+        stage_rows(lds, vt_write, x, v[x], shift);
+        scores_rows(s, x, k[x], shift, st);
+      }
+    };
+    request(begin);
+    const int full_end = min(pre_end, u.n_keys / 32);   // (only the list's last tile can be a partial one)
+    for (int tile = begin; tile < full_end; ++tile) {
+      f32x4 s[RB][2];
+      consume(s, 31);
+      request(tile + 1);
+      __builtin_amdgcn_sched_barrier(0);
       wave_order();
-      if ((tile + 1) * 32 <= n_keys)
-        attend<D, RB, TILE_FULL>(st, s, vt, p.scale_log2, tile * 32, n_keys, lane);
-      else
-        attend<D, RB, TILE_TAIL>(st, s, vt, p.scale_log2, tile * 32, n_keys, lane);
+      attend_rows<D, RB, TILE_FULL>(st, s, lds, vt_read, p.scale_log2, tile * 32, u.n_keys, lane);
+      wave_order();
+    }
+    if (full_end < pre_end) {
+      f32x4 s[RB][2];
+      consume(s, u.n_keys - 1 - full_end * 32);
+      wave_order();
+      attend_rows<D, RB, TILE_TAIL>(st, s, lds, vt_read, p.scale_log2, full_end * 32, u.n_keys, lane);
       wave_order();
     }
   }
   // the branch's own tokens
   for (int tile = max(begin, n_tiles); tile < end; ++tile) {
-    const int first = own0 + (tile - n_tiles) * 32;
-    const size_t row = ((size_t)b * p.gamma * p.L + min(first + ln, own_end - 1)) * p.Hkv + hk;
-    Raw<FMT_BF16, D> k, v;
-    load_half(k, p.k_branch, nullptr, row, h);
-    load_half(v, p.v_branch, nullptr, row, h);
-    stage_v(vt, v, ln, h);
-    f32x16 s[RB];
-    scores(s, k, st);
-    wave_order();
-    attend<D, RB, TILE_OWN>(st, s, vt, p.scale_log2, first, own_end, lane);
+    const int first = u.own0 + (tile - n_tiles) * 32;
+    f32x4 s[RB][2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const size_t row = ((size_t)u.b * p.gamma * p.L + min(first + x * 16 + n, u.own_end - 1)) * p.Hkv + u.hk;
+      Quarter<FMT_BF16, D> r;
+      load_quarter(r, p.v_branch, nullptr, row, quarter);
+      stage_rows(lds, vt_write, x, r, 0);
+      wave_order();   // (one half row in registers at a time)
+      load_quarter(r, p.k_branch, nullptr, row, quarter);
+      scores_rows(s, x, r, 0, st);
+      wave_order();
+    }
+    attend_rows<D, RB, TILE_OWN>(st, s, lds, vt_read, p.scale_log2, first, u.own_end, lane);
     wave_order();
   }
 
-  // fold the four wavefronts: common maximum, then the accumulators pairwise through LDS
+  // fold the wavefronts: common maximum, then the accumulators through LDS, half of those left at a time
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    st.l[rb] = xhalf_sum(st.l[rb]);
-    if (h == 0) fold_ml[wave][rb * 32 + ln][0] = st.m[rb], fold_ml[wave][rb * 32 + ln][1] = st.l[rb];
+    st.l[rb] = quarter_sum(st.l[rb]);
+    if (quarter == 0) fold_ml[wave][rb * 16 + n][0] = st.m[rb], fold_ml[wave][rb * 16 + n][1] = st.l[rb];
   }
   __syncthreads();  // (also: every wavefront is done with its V tile)
   float m_all[RB], l_all[RB];
@@ -341,88 +480,331 @@ __global__ __launch_bounds__(256, RB == 1 && D <= 128 ? 2 : 1) void attn_blocks_
   for (int rb = 0; rb < RB; ++rb) {
     m_all[rb] = -INFINITY, l_all[rb] = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m_all[rb] = fmaxf(m_all[rb], fold_ml[w][rb * 32 + ln][0]);
+    for (int w = 0; w < NW; ++w) m_all[rb] = fmaxf(m_all[rb], fold_ml[w][rb * 16 + n][0]);
     const float base = m_all[rb] == -INFINITY ? 0.f : m_all[rb];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      l_all[rb] += fold_ml[w][rb * 32 + ln][1] * __builtin_amdgcn_exp2f(fold_ml[w][rb * 32 + ln][0] - base);
+    for (int w = 0; w < NW; ++w)
+      l_all[rb] += fold_ml[w][rb * 16 + n][1] * __builtin_amdgcn_exp2f(fold_ml[w][rb * 16 + n][0] - base);
     const float f = __builtin_amdgcn_exp2f(st.m[rb] - base);
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) st.o[rb][db][j] *= f;
+    for (int db = 0; db < D / 16; ++db) st.o[rb][db] *= f;
   }
-  constexpr int kOne = RB * (D / 32) * 16 * 64;  // floats of one wavefront's accumulators
-  float *buf = (float *)lds;
-  auto put = [&](float *dst) __attribute__((always_inline)) {
+  f32x4 *buf = (f32x4 *)lds;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+  for (int left = NW; left > 1; left /= 2) {
+    if (wave >= left / 2 && wave < left) {
+      f32x4 *dst = buf + (wave - left / 2) * (kOne / 4) + lane;
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
+      for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) dst[((rb * (D / 32) + db) * 16 + j) * 64 + lane] = st.o[rb][db][j];
-  };
-  auto add = [&](const float *src) __attribute__((always_inline)) {
+        for (int db = 0; db < D / 16; ++db) dst[(rb * (D / 16) + db) * 64] = st.o[rb][db];
+    }
+    __syncthreads();
+    if (wave < left / 2) {
+      const f32x4 *src = buf + wave * (kOne / 4) + lane;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+      for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) st.o[rb][db][j] += src[((rb * (D / 32) + db) * 16 + j) * 64 + lane];
-  };
-  if (wave & 1) put(buf + (wave >> 1) * kOne);
-  __syncthreads();
-  if (!(wave & 1)) add(buf + (wave >> 1) * kOne);
-  __syncthreads();
-  if (wave == 2) put(buf);
-  __syncthreads();
+        for (int db = 0; db < D / 16; ++db) st.o[rb][db] += src[(rb * (D / 16) + db) * 64];
+    }
+    if (left > 2) __syncthreads();
+  }
   if (wave != 0) return;
-  add(buf);
-
-  const size_t all_rows = (size_t)p.B * p.n_rows;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const int r = r0 + rb * 32 + ln;
-    if (r >= n_group_rows) continue;
-    const size_t grow = (size_t)b * p.n_rows + (size_t)(tok0 + r / p.G) * p.Hq + hk * p.G + r % p.G;
-    if (p.part_o) {
-      const size_t prow = split * all_rows + grow;
-      if (h == 0) *(f32x2 *)(p.part_ml + prow * 2) = f32x2{m_all[rb], l_all[rb]};
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          *(f32x4 *)(p.part_o + prow * D + db * 32 + q * 8 + h * 4) =
-              f32x4{st.o[rb][db][4 * q], st.o[rb][db][4 * q + 1], st.o[rb][db][4 * q + 2], st.o[rb][db][4 * q + 3]};
-      continue;
-    }
+    const int r = u.r0 + rb * 16 + n;
+    if (r >= u.n_rows) continue;
+    const size_t grow = out_row(p, u, r);
+    if (quarter == 0) put_sums(p, u, grow, m_all[rb], l_all[rb]);
     const float inv = 1.0f / l_all[rb];
-    if (p.lse && h == 0) p.lse[grow] = 0.69314718055994530942f * (m_all[rb] + __builtin_log2f(l_all[rb]));
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) put_out(p, u, grow, db * 16 + quarter * 4, D, st.o[rb][db], inv);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- many rows
+
+// A tile on its way from memory to LDS, K and V as wavefront loads of 64 x 16 bytes that the NW wavefronts of the workgroup take
+// in turn.  Quantised rows pass through registers: lane (key n of 16, chunk quarter + 4 i), so that one load takes whole rows
+// of 64 bytes and more, and one store instruction one piece of 16 keys.  bf16 rows go to LDS at once: lane l of a load fills
+// place l of 64 pieces, so it fetches the piece that belongs there.
+template <int FMT, int D, int KEYS, int NW>
+struct Stage {
+  static constexpr int kElems = FMT == FMT_BF16 ? 8 : FMT == FMT_MX8 ? 16 : 32;   // of 16 bytes
+  static constexpr int kChunks = D / kElems;                                      // of a row
+  static constexpr int kGroups = kChunks < 4 ? 1 : kChunks / 4;                   // wavefront loads per 16 keys
+  static constexpr int kTensor = FMT == FMT_BF16 ? KEYS * kChunks / 64 : KEYS / 16 * kGroups;   // of K, and of V
+  static constexpr int kLoads = (2 * kTensor + NW - 1) / NW;
+  u32x4 w[FMT == FMT_BF16 ? 1 : kLoads];
+  uint32_t e[FMT == FMT_BF16 ? 1 : kLoads];
+};
+
+template <int FMT, int D, int KEYS, int NW, typename F>
+__device__ __forceinline__ void stage_load(Stage<FMT, D, KEYS, NW> &g, const uint8_t *lds, const void *kb, const void *vb, const uint8_t *kx,
+                                           const uint8_t *vx, F row_of) {
+  using S = Stage<FMT, D, KEYS, NW>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+  for (int i = 0; i < S::kLoads; ++i) {
+    const int load = wave + i * NW, which = load >= S::kTensor ? 1 : 0, at = load - which * S::kTensor;
+    if (load >= 2 * S::kTensor) continue;
+    const uint8_t *base = (const uint8_t *)(which ? vb : kb);
+    if constexpr (FMT == FMT_BF16) {
+      constexpr int kRows = 64 / S::kChunks;
+      const int first = at * kRows, key = first + lane / S::kChunks;
+      load_lds16(base + (row_of(key) * S::kChunks + ((lane % S::kChunks) ^ swizzle<D>(key))) * 16,
+                 lds_address(lds) + (which * KEYS + first) * D * 2);
+    } else {
+      const int key = at / S::kGroups * 16 + (lane & 15), chunk = min((lane >> 4) + 4 * (at % S::kGroups), S::kChunks - 1);
+      const size_t row = row_of(key);
+      g.w[i] = *(const u32x4 *)(base + (row * S::kChunks + chunk) * 16);
+      g.e[i] = *(const uint32_t *)((which ? vx : kx) + ((row * (D / 32) + chunk * S::kElems / 32) & ~(size_t)3));
+    }
+  }
+}
+
+// Before the barrier behind which the tile is read.  last: the tile's last key that exists (those behind it repeat it).
+template <int FMT, int D, int KEYS, int NW>
+__device__ __forceinline__ void stage_store(const Stage<FMT, D, KEYS, NW> &g, uint8_t *lds, int last) {
+  using S = Stage<FMT, D, KEYS, NW>;
+  if constexpr (FMT == FMT_BF16) {
+    wait_loads();
+  } else {
+    constexpr int kPieces = S::kElems / 8;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < S::kLoads; ++i) {
+      const int load = wave + i * NW, which = load >= S::kTensor ? 1 : 0, at = load - which * S::kTensor;
+      if (load >= 2 * S::kTensor) continue;
+      const int key = at / S::kGroups * 16 + (lane & 15), chunk = (lane >> 4) + 4 * (at % S::kGroups);
+      if (S::kChunks < 4 && chunk >= S::kChunks) continue;   // (a D = 64 row of fp4 has two chunks)
+      const uint32_t w[4] = {g.w[i][0], g.w[i][1], g.w[i][2], g.w[i][3]};
+      // (a block's rows begin at a multiple of 16, so the key says where in its word an exponent is)
+      const uint32_t e = (g.e[i] >> (((min(key, last) * (D / 32) + chunk * S::kElems / 32) & 3) * 8)) & 0xffu;
+      const int row = key * D * 2 + (((chunk * kPieces) ^ swizzle<D>(key)) << 4);
+      uint8_t *to = lds + which * KEYS * D * 2;
+#pragma unroll
+      for (int t = 0; t < kPieces; ++t) *(u32x4 *)(to + (row ^ (t << 4))) = widen8<FMT>(w + t * kWords8<FMT>, exp_scale(e));
+    }
+  }
+}
+
+template <int D>
+struct TileRows {
+  bf16x8 q[D / 16];            // row ln: d = 16 t + 8 h ..
+  f32x16 o[D / 32];
+  float m, l;
+  int tok, start;
+};
+
+// A wavefront's NB blocks of 32 keys of a tile in LDS: scores, probabilities, product with V.  kt, vt: offsets of the lane's K
+// and V operands in LDS; first: the first key.
+template <int D, int NB, int MASK>
+__device__ __forceinline__ void attend_tile(TileRows<D> &st, const uint8_t *lds, int kt, int vt, float scale_log2, int first, int limit, int lane) {
+  const int h = lane >> 5;
+  f32x16 s[NB];
+#pragma unroll
+  for (int kb = 0; kb < NB; ++kb) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) s[kb][j] = 0.f;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+      const bf16x8 kf = *(const bf16x8 *)(lds + (kt ^ (t << 5)) + kb * 32 * D * 2);
+      s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, st.q[t], s[kb], 0, 0, 0);
+    }
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int key = first + kb * 32 + (j >> 2) * 8 + h * 4 + (j & 3);
+      if constexpr (MASK == TILE_TAIL) {
+        if (key >= limit) s[kb][j] = -INFINITY;
+      } else if constexpr (MASK == TILE_OWN) {
+        if (key > st.tok || key < st.start) s[kb][j] = -INFINITY;
+      }
+      top = fmaxf(top, s[kb][j]);
+    }
+  top = xhalf_max(top) * scale_log2;
+  const bool up = top > st.m + kRaise;
+  const float m = up ? top : st.m;
+  if (__builtin_amdgcn_ballot_w64(up)) {
+    const float alpha = up ? __builtin_amdgcn_exp2f(st.m - m) : 1.0f;
+    st.l *= alpha;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4 x = f32x4{st.o[rb][db][4 * q], st.o[rb][db][4 * q + 1], st.o[rb][db][4 * q + 2], st.o[rb][db][4 * q + 3]} * inv;
-        const size_t at = grow * D + db * 32 + q * 8 + h * 4;
-        if (p.out_f32)
-          *(f32x4 *)((float *)p.out + at) = x;
-        else
-          *(u32x2 *)((uint8_t *)p.out + at * 2) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-      }
+      for (int j = 0; j < 16; ++j) st.o[db][j] *= alpha;
   }
+  st.m = m;
+  const float base = m == -INFINITY ? 0.f : m;  // no key seen yet: every score is -inf
+  float sum = 0.f;
+#pragma unroll
+  for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      u32x4 pw;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][8 * c + 2 * x], scale_log2, -base));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][8 * c + 2 * x + 1], scale_log2, -base));
+        sum += p0 + p1;
+        pw[x] = pack_bf16(p0, p1);
+      }
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+      // V^T operands: lane (d, h) takes keys 16 c + 4 h + 0..3 and 8 more, the order of the probabilities
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const uint8_t *at = lds + (kb * 32 + 16 * c) * D * 2;
+        const bf16x8 vf = read_transposed(at + (vt ^ (db << 6)), at + (vt ^ (db << 6) ^ 32) + 8 * D * 2);
+        st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, st.o[db], 0, 0, 0);
+      }
+    }
+  st.l += sum;
 }
+
+// RW wavefronts side by side along the rows, KS along the keys of a tile.
+template <int FMT, int D, int RW, int KS>
+__global__ __launch_bounds__(64 * RW * KS, 2) void attn_tile_kernel(const SparseParams p) {
+  constexpr int KEYS = D == 256 ? 32 : 64, NB = KEYS / 32 / KS, NW = RW * KS;
+  static_assert(NB >= 1, "every wavefront has keys of a tile");
+  constexpr int kTileBytes = KEYS * D * 2;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kTileBytes];  // two buffers of a K and a V tile
+  __shared__ Places places;
+  __shared__ float fold_ml[RW * 32][2];
+  static_assert(KS == 1 || RW * (D / 32) * 16 * 64 * 4 <= 4 * kTileBytes, "the accumulators of the upper keys fit");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ln = lane & 31, h = lane >> 5;
+  const int row_wave = wave % RW, key_wave = wave / RW;
+  Unit u;
+  if (!find_unit<RW * 32, KEYS, 64 * NW>(p, u, places)) return;
+  const int n_tiles = u.n_tiles, begin = u.begin, end = u.end, pre_end = min(end, n_tiles);
+
+  TileRows<D> st;
+  const int r = u.r0 + row_wave * 32 + ln, r_in = min(r, u.n_rows - 1);
+  {
+    const uint8_t *src = (const uint8_t *)p.q + out_row(p, u, r_in) * D * 2 + h * 16;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) st.q[t] = *(const bf16x8 *)(src + t * 32);
+    st.tok = u.tok0 + r_in / p.G, st.start = st.tok / p.L * p.L;
+    st.m = -INFINITY, st.l = 0.f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) st.o[db][j] = 0.f;
+  }
+  const bool any_row = u.r0 + row_wave * 32 < u.n_rows;  // (a wavefront without rows only helps to stage)
+  // the lane's operands in a buffer (a row's pieces are permuted inside the row, whose size is a power of two: XOR)
+  const int i = lane & 15, read_key = 4 * h + (i >> 2), my_keys = key_wave * NB * 32;
+  const int kt = (my_keys + ln) * D * 2 + ((h ^ swizzle<D>(ln)) << 4);
+  const int vt = kTileBytes + (my_keys + read_key) * D * 2 +
+                 (((2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ swizzle<D>(read_key)) << 4) + (i & 1) * 8;
+  __syncthreads();
+
+  if (begin < pre_end) {
+    Stage<FMT, D, KEYS, NW> g;
+    auto load = [&](int tile, const uint8_t *to) __attribute__((always_inline)) {
+      stage_load(g, to, p.k_cache, p.v_cache, p.k_exp, p.v_exp, [&](int in_tile) __attribute__((always_inline)) {
+        const int key = min(tile * KEYS + in_tile, u.n_keys - 1);
+        const int blk = places.place[(key >> p.block_shift) - u.slot0];
+        return (((size_t)blk * p.Hkv + u.hk) << p.block_shift) + (key & ((1 << p.block_shift) - 1));
+      });
+    };
+    load(begin, lds);
+    stage_store(g, lds, u.n_keys - 1 - begin * KEYS);
+    __syncthreads();
+    const int full_end = min(pre_end, u.n_keys / KEYS);   // (only the list's last tile can be a partial one)
+    int at = 0;
+    for (int tile = begin; tile < full_end; ++tile, at ^= 2 * kTileBytes) {
+      uint8_t *other = lds + (at ^ (2 * kTileBytes));
+      if (tile + 1 < pre_end) load(tile + 1, other);
+      if (any_row) attend_tile<D, NB, TILE_FULL>(st, lds + at, kt, vt, p.scale_log2, tile * KEYS + my_keys, u.n_keys, lane);
+      if (tile + 1 < pre_end) stage_store(g, other, u.n_keys - 1 - (tile + 1) * KEYS);
+      __syncthreads();
+    }
+    if (full_end < pre_end) {
+      if (any_row) attend_tile<D, NB, TILE_TAIL>(st, lds + at, kt, vt, p.scale_log2, full_end * KEYS + my_keys, u.n_keys, lane);
+      __syncthreads();
+    }
+  }
+  // the branches' own tokens
+  for (int tile = max(begin, n_tiles); tile < end; ++tile) {
+    const int first = u.own0 + (tile - n_tiles) * KEYS;
+    Stage<FMT_BF16, D, KEYS, NW> g;
+    stage_load(g, lds, p.k_branch, p.v_branch, nullptr, nullptr, [&](int in_tile) __attribute__((always_inline)) {
+      return ((size_t)u.b * p.gamma * p.L + min(first + in_tile, u.own_end - 1)) * p.Hkv + u.hk;
+    });
+    stage_store(g, lds, 0);
+    __syncthreads();
+    if (any_row) attend_tile<D, NB, TILE_OWN>(st, lds, kt, vt, p.scale_log2, first + my_keys, u.own_end, lane);
+    __syncthreads();
+  }
+
+  float l = xhalf_sum(st.l), m = st.m;
+  if constexpr (KS == 2) {
+    // the two halves of the keys: common maximum, then the sum of the accumulators through LDS
+    float *buf = (float *)lds + row_wave * (D / 32) * 16 * 64 + lane;
+    if (key_wave == 1) {
+      if (h == 0) fold_ml[row_wave * 32 + ln][0] = m, fold_ml[row_wave * 32 + ln][1] = l;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) buf[(db * 16 + j) * 64] = st.o[db][j];
+    }
+    __syncthreads();
+    if (key_wave == 1) return;
+    const float m1 = fold_ml[row_wave * 32 + ln][0], l1 = fold_ml[row_wave * 32 + ln][1];
+    const float m_all = fmaxf(m, m1), base = m_all == -INFINITY ? 0.f : m_all;
+    const float f0 = __builtin_amdgcn_exp2f(m - base), f1 = __builtin_amdgcn_exp2f(m1 - base);
+    m = m_all, l = l * f0 + l1 * f1;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) st.o[db][j] = st.o[db][j] * f0 + buf[(db * 16 + j) * 64] * f1;
+  }
+  if (r >= u.n_rows) return;
+  const float inv = 1.0f / l;
+  const size_t grow = out_row(p, u, r);
+  if (h == 0) put_sums(p, u, grow, m, l);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      put_out(p, u, grow, db * 32 + q * 8 + h * 4, D,
+              f32x4{st.o[db][4 * q], st.o[db][4 * q + 1], st.o[db][4 * q + 2], st.o[db][4 * q + 3]}, inv);
+}
+
+// ---------------------------------------------------------------------------------------------------- launch
 
 template <int FMT, int D>
 hipError_t launch(const SparseParams &p, hipStream_t stream) {
   const int64_t units = (int64_t)p.B * p.n_groups * p.n_row_tiles * p.Hkv;
-  const dim3 grid((unsigned)(units * p.n_split)), block(64 * kWaves);
-  if (p.tile_rows == 32) {
-    hipLaunchKernelGGL((attn_blocks_kernel<FMT, D, 1>), grid, block, 0, stream, p);
-  } else {
-    if constexpr (D <= 128)
-      hipLaunchKernelGGL((attn_blocks_kernel<FMT, D, 2>), grid, block, 0, stream, p);
-    else
-      return hipErrorInvalidValue;
+  const dim3 grid((unsigned)(units * p.n_split)), block(64 * p.waves);
+  switch (p.tile_rows * 100 + p.waves) {
+    case 1604: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 1, 4>), grid, block, 0, stream, p); break;
+    case 1608: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 1, 8>), grid, block, 0, stream, p); break;
+    case 3204: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 2, 4>), grid, block, 0, stream, p); break;
+    case 12804:
+      if constexpr (D == 256) {
+        hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 4, 1>), grid, block, 0, stream, p);
+        break;
+      } else {
+        return hipErrorInvalidValue;
+      }
+    default:
+      if constexpr (D < 256) {
+        switch (p.tile_rows * 100 + p.waves) {
+          case 1616: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 1, 16>), grid, block, 0, stream, p); break;
+          case 3208: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 2, 8>), grid, block, 0, stream, p); break;
+          case 6404: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 2, 2>), grid, block, 0, stream, p); break;
+          case 9606: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 3, 2>), grid, block, 0, stream, p); break;
+          case 12808: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 4, 2>), grid, block, 0, stream, p); break;
+          default: return hipErrorInvalidValue;
+        }
+        break;
+      } else {
+        return hipErrorInvalidValue;
+      }
   }
   return hipGetLastError();
 }
@@ -440,8 +822,6 @@ hipError_t launch_d(const SparseParams &p, hipStream_t stream) {
 }  // namespace
 
 int attn_blocks_max_slots() { return kMaxSlots; }
-int attn_blocks_tile_rows(int D, int rows) { return D <= 128 && rows > 32 ? 64 : 32; }
-
 hipError_t launch_attn_blocks(const SparseParams &p, int format, hipStream_t stream) {
   ProfileScope scope(SLOT_ATTN_BLOCKS, stream);
   switch (format) {

@@ -108,40 +108,84 @@ la_status plan_select(const la_attn_desc *d, const la_select_desc *s, const int3
 }
 
 struct SparsePlan {
-  int n_groups, tile_rows, n_row_tiles, n_split;
+  int n_groups, tile_rows, n_row_tiles, waves, n_split;
   size_t part_o_bytes, part_ml_bytes;
 };
 
+// Kernel shapes of the attention over blocks: rows per unit, wavefronts per workgroup, keys per tile, and microseconds per tile of
+// a workgroup that has its CU to itself (latency) and of one of several that share it (busy, before the memory's share).
+struct SparseShape {
+  int rows, waves, keys;
+  double latency, busy;
+};
+constexpr SparseShape kShapes[] = {
+    {16, 4, 32, 0.26, 0.15}, {16, 8, 32, 0.15, 0.13}, {32, 4, 32, 0.30, 0.20}, {32, 8, 32, 0.17, 0.20},
+    {64, 4, 64, 1.30, 0.83}, {96, 6, 64, 1.20, 1.20}, {128, 8, 64, 1.30, 1.30},
+    {128, 4, 32, 2.0, 2.0},  // (head dimension 256)
+};
+bool shape_fits(const SparseShape &s, int D, int64_t rows) {
+  if (D == 256) return rows <= 16 ? s.rows == 16 : rows <= 32 ? s.rows == 32 && s.waves == 4 : s.rows == 128 && s.waves == 4;
+  if (s.keys == 32 && s.rows == 128) return false;
+  return rows <= 16 ? s.rows == 16 : rows <= 32 ? s.rows == 32 : rows <= 64 ? s.rows == 64 : s.rows >= 64;
+}
+
+// Which shape runs a call and over how many workgroups a unit's keys are split, from a simple model in microseconds (constants
+// fitted to the figures in attn_blocks.hip): what the workgroups of all units take, shared out over the CUs, or the longest
+// of them, whichever is more, and the merge of the partial results.
 la_status plan_sparse(const la_attn_desc *d, const la_select_desc *s, const int32_t *prefix_lens_host, SparsePlan *plan) {
   la_status st = validate(d);
   if (st != LA_OK) return st;
   if (s && (st = validate_select(d, s)) != LA_OK) return st;
   int64_t longest = 0;
   if ((st = check_prefixes(d, prefix_lens_host, &longest)) != LA_OK) return st;
-  const int G = d->num_q_heads / d->num_kv_heads;
+  const int G = d->num_q_heads / d->num_kv_heads, D = d->head_dim;
   const int64_t rows = (int64_t)(s ? s->group_len : d->gamma * d->branch_len) * G;   // of a group
-  plan->n_groups = s ? d->gamma * num_groups(d, s) : 1;
-  plan->tile_rows = attn_blocks_tile_rows(d->head_dim, (int)rows);
-  plan->n_row_tiles = (int)((rows + plan->tile_rows - 1) / plan->tile_rows);
-  const int64_t units = (int64_t)d->num_requests * plan->n_groups * plan->n_row_tiles * d->num_kv_heads;
-  if (units > kMaxUnits) return LA_ERR_UNSUPPORTED;
-  int64_t keys = longest;
-  if (s && (int64_t)s->max_blocks * d->block_size < keys) keys = (int64_t)s->max_blocks * d->block_size;
-  const int64_t tiles = (keys + 31) / 32 + ((int64_t)d->branch_len + plan->tile_rows) / 32 + 2;  // and own tokens
-  // as many workgroups per unit as fill the chip twice, each wavefront with at least two tiles
-  int64_t n = (2 * (int64_t)num_cus() + units - 1) / units;
-  const int64_t most = (tiles + 7) / 8;
-  n = n < most ? n : most;
-  // the blocks of a workgroup's tiles have to fit its table (a range need not begin at a block's first key)
-  const int64_t fit = ((int64_t)attn_blocks_max_slots() - 2) * d->block_size / 32 - 2;
-  const int64_t least = (tiles + fit - 1) / fit;
-  n = n > least ? n : least;
-  n = n < 1 ? 1 : n;
-  if (units * n > kMaxUnits) return LA_ERR_UNSUPPORTED;
-  plan->n_split = (int)n;
+  const int64_t listed = s ? (int64_t)s->max_blocks * d->block_size : (int64_t)1 << 30;
+  int64_t all_keys = 0;
+  for (int b = 0; b < d->num_requests; ++b) all_keys += prefix_lens_host[b] < listed ? prefix_lens_host[b] : listed;
+  const int64_t most_keys = longest < listed ? longest : listed;
   const size_t all_rows = (size_t)d->num_requests * d->gamma * d->branch_len * d->num_q_heads;
-  plan->part_o_bytes = n > 1 ? align_up((size_t)n * all_rows * d->head_dim * sizeof(float)) : 0;
-  plan->part_ml_bytes = n > 1 ? align_up((size_t)n * all_rows * 2 * sizeof(float)) : 0;
+  const double row_bytes = 2.0 * (d->kv_dtype == LA_BF16 ? 2.0 * D : d->kv_dtype == LA_MXFP8_E4M3 ? D * 33.0 / 32 : D * 17.0 / 32);
+  plan->n_groups = s ? d->gamma * num_groups(d, s) : 1;
+  const int cus = num_cus();
+  double best = -1.0;
+  for (const SparseShape &shape : kShapes) {
+    if (!shape_fits(shape, D, rows)) continue;
+    const int64_t row_tiles = (rows + shape.rows - 1) / shape.rows;
+    const int64_t per_request = (int64_t)plan->n_groups * row_tiles * d->num_kv_heads, units = per_request * d->num_requests;
+    if (units > kMaxUnits) return LA_ERR_UNSUPPORTED;
+    // tiles of the longest request's units, and of all (own tokens of the branches that a unit's rows belong to)
+    const int64_t own = ((int64_t)d->branch_len + shape.rows) / shape.keys + 2;
+    const int64_t most = (most_keys + shape.keys - 1) / shape.keys + own;
+    const double tiles = (double)all_keys / shape.keys + (double)d->num_requests * own;
+    // the blocks of a workgroup's tiles have to fit its table (a range need not begin at a block's first key)
+    const int64_t fit = ((int64_t)attn_blocks_max_slots() - 2) * d->block_size / shape.keys - 2;
+    const int64_t least = (most + fit - 1) / fit;
+    if (units * least > kMaxUnits) return LA_ERR_UNSUPPORTED;
+    // all CUs stream at 5 TB/s between them
+    const double scale = D / 128.0, stream = shape.keys * row_bytes * cus / 5.0e6;
+    const double busy = shape.busy * scale > stream ? shape.busy * scale : stream;
+    const double alone = shape.latency * scale > busy ? shape.latency * scale : busy;
+    const int64_t slots = most / (shape.keys == 32 ? shape.waves : 1);   // a tile at least for every wavefront
+    for (int64_t n = least; n == least || (n <= slots && n <= 64 && units * n <= 4 * (int64_t)cus); ++n) {
+      const double start = 1.5, longest_us = (double)most / (double)n * alone + start;
+      const double all_us = (double)per_request / cus * (tiles * busy + (double)(n * d->num_requests) * start);
+      const double merge_us = n > 1 ? 3.0 + (double)(n * all_rows) * (D + 2) * 8.0 / 3.0e6 : 0.0;
+      // units of one length come in whole rounds
+      const int64_t rounds = (units * n + cus - 1) / cus;
+      const double even_us = (double)rounds * ((double)most / (double)n * busy + start);
+      const bool even = most_keys * d->num_requests == all_keys;
+      double us = even ? even_us : all_us + 0.5 * longest_us;
+      us = (us > longest_us ? us : longest_us) + merge_us;
+      if (best < 0.0 || us < best) {
+        best = us;
+        plan->tile_rows = shape.rows, plan->waves = shape.waves, plan->n_row_tiles = (int)row_tiles, plan->n_split = (int)n;
+      }
+    }
+  }
+  const size_t n = (size_t)plan->n_split;
+  plan->part_o_bytes = n > 1 ? align_up(n * all_rows * D * sizeof(float)) : 0;
+  plan->part_ml_bytes = n > 1 ? align_up(n * all_rows * 2 * sizeof(float)) : 0;
   return LA_OK;
 }
 
@@ -297,7 +341,7 @@ la_status la_verify_attention_sparse(const la_attn_desc *desc, const la_select_d
   p.gamma = desc->gamma, p.L = desc->branch_len;
   p.block_shift = __builtin_ctz((unsigned)desc->block_size), p.max_blocks = desc->max_blocks_per_request;
   p.max_sel = sel ? sel->max_blocks : 0, p.group_len = sel ? sel->group_len : 0;
-  p.n_groups = plan.n_groups, p.tile_rows = plan.tile_rows, p.n_row_tiles = plan.n_row_tiles;
+  p.n_groups = plan.n_groups, p.tile_rows = plan.tile_rows, p.n_row_tiles = plan.n_row_tiles, p.waves = plan.waves;
   p.n_rows = desc->gamma * desc->branch_len * desc->num_q_heads;
   p.n_split = plan.n_split, p.out_f32 = desc->out_dtype == LA_F32;
   p.scale_log2 = desc->softmax_scale * 1.44269504088896340736f;

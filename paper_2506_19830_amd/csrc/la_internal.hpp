@@ -258,13 +258,12 @@ struct SparseParams {
   float *lse;
   int B, Hq, Hkv, G, D, gamma, L, block_shift, max_blocks;
   int max_sel, group_len, n_groups;   // n_groups: groups of one request
-  int tile_rows, n_row_tiles;         // of one group
+  int tile_rows, n_row_tiles, waves;  // kernel shape: rows per unit, wavefronts per workgroup (see block_api.hip)
   int n_rows;                         // gamma * L * Hq
   int n_split, out_f32;
   float scale_log2;
 };
 int attn_blocks_max_slots();                       // block ids a workgroup can hold
-int attn_blocks_tile_rows(int D, int rows);        // rows per unit for groups of `rows` rows
 hipError_t launch_attn_blocks(const SparseParams &p, int format, hipStream_t stream);
 
 // ----------------------------------------------------------------------------
