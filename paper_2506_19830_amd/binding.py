@@ -208,12 +208,13 @@ def status_string(status: int) -> str:
     return load().la_status_string(int(status)).decode()
 
 
-def _ptr(t: Optional[torch.Tensor]) -> ctypes.c_void_p:
-    return ctypes.c_void_p(0 if t is None else t.data_ptr())
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
 
 
-def _stream() -> ctypes.c_void_p:
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+def _stream() -> int:
+    # the current stream's handle without a Stream object around it (2.9 -> 0.3 us of every call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def make_attn_desc(*, num_requests, num_q_heads, num_kv_heads, head_dim, gamma, branch_len, block_size,
