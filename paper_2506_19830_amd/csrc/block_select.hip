@@ -48,46 +48,104 @@ __device__ __forceinline__ void split_signs(const u32x4 q, u32x4 &neg, u32x4 &po
   }
 }
 
+// 16 bytes per lane from memory to consecutive places in LDS, without registers in between.
+__device__ __forceinline__ void load_lds16(const uint8_t *src, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds_addr) : "m0");
+}
+// Until at most N of the wavefront's loads are under way.  (The fences: the compiler does not see the loads' writes to LDS, so
+// reads must not be moved over the wait.)
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0070 | 0x0F00);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
+}
+
 // A wavefront keeps the bounds of 32 blocks (NB tiles of them) in registers as matrix operands while query rows pass, 32 at a
 // time.  Groups of at most SLOT rows share such a tile of rows: with rows 8 q .. 8 q + 7 in registers 4 q .. 4 q + 3 of the
 // result, the largest of a group's rows is a maximum over registers and the two halves of the wavefront.  Larger groups take
-// several tiles (SLOT = 32).
+// several tiles (SLOT = 32), which the four wavefronts of a workgroup share in LDS.
+//   Everything comes from memory in whole rows and is taken apart in LDS: operands read from memory directly, 16 bytes of 32
+// rows per instruction, kept the cache's tag look-ups busy (steps of 320 rows, 2048 blocks: 34 -> 26 us).  A row's 16-byte pieces lie permuted by the row's number, so that the reads of one piece of 16 rows miss no bank.
 template <int D, int SLOT, int NB>
 __global__ __launch_bounds__(256) void block_score_kernel(const SelectParams p) {
   constexpr int T = D / 16, kShare = 32 / SLOT, kRegs = SLOT / 2;  // groups of a row tile; registers of a group
-  const int lane = threadIdx.x & 63, ln = lane & 31, h = lane >> 5;
-  const int tile = (blockIdx.x * 4 + (threadIdx.x >> 6)) * NB;
+  constexpr int kPieces = D / 8, kMask = kPieces < 16 ? kPieces - 1 : 15;   // 16-byte pieces of a query row
+  constexpr int kBoundBytes = 32 * 4 * D, kTileBytes = 32 * 2 * D;
+  constexpr int kRing = 4, kPerWave = kTileBytes / 1024 / 4;        // query tiles in LDS; loads of a wavefront per tile
+  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kBoundBytes];
+  static_assert(kRing * kTileBytes <= 4 * kBoundBytes, "the query tiles take the place of the bounds");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ln = lane & 31, h = lane >> 5;
   uint32_t id = blockIdx.y + blockIdx.z * 65535u;
   if (id >= (uint32_t)(p.B * p.score_chunks * p.Hkv)) return;
   const int hk = (int)(id % (uint32_t)p.Hkv);
   id /= (uint32_t)p.Hkv;
   const int chunk = (int)(id % (uint32_t)p.score_chunks), b = (int)(id / (uint32_t)p.score_chunks);
-  const int n = prefix_blocks(p, b);
-  if (n <= p.max_sel || tile * 32 >= n) return;  // all blocks are taken / no such blocks
+  const int tile = (blockIdx.x * 4 + wave) * NB;
+  const uint32_t bounds_at = lds_address(lds) + wave * kBoundBytes;
+  const int32_t *table = p.block_tables ? p.block_tables + (size_t)b * p.max_blocks : nullptr;
   u32x4 lo[NB][T], hi[NB][T];
+  // the table's entries are asked for together with the prefix's length (those behind it are not used); blocks behind the last
+  // repeat the last one, or where that is in another tile block 0 of the request
+  int blk[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    const int lb = min((tile + nb) * 32 + ln, n - 1);
-    const int blk = p.block_tables ? p.block_tables[(size_t)b * p.max_blocks + lb] : b * p.max_blocks + lb;
-    const uint8_t *src = (const uint8_t *)p.k_bounds + ((size_t)blk * p.Hkv + hk) * 4 * D + h * 16;
+    const int lb = min((tile + nb) * 32 + ln, p.max_blocks - 1);
+    blk[nb] = table ? table[lb] : b * p.max_blocks + lb;
+  }
+  const int n = prefix_blocks(p, b);
+  if (n <= p.max_sel || blockIdx.x * 4 * NB * 32 >= (uint32_t)n) return;  // all blocks are taken / no such blocks
 #pragma unroll
-    for (int t = 0; t < T; ++t) lo[nb][t] = *(const u32x4 *)(src + t * 32), hi[nb][t] = *(const u32x4 *)(src + 2 * D + t * 32);
+  for (int nb = 0; nb < NB; ++nb) {
+    const int last = n - 1 - (tile + nb) * 32;   // of the tile's blocks; negative: no such tile, which then repeats block 0
+    if (last < 0) blk[nb] = table ? table[0] : b * p.max_blocks;
+    const int edge = __shfl(blk[nb], min(max(last, 0), 31));
+    if (ln > last) blk[nb] = edge;
   }
   const int per_req = p.gamma * p.n_groups;
-  const int first = (int)((int64_t)chunk * p.score_tiles / p.score_chunks) * kShare;
-  const int end = min((int)((int64_t)(chunk + 1) * p.score_tiles / p.score_chunks) * kShare, per_req);
-
+  const int first = chunk * p.score_groups, end = min(first + p.score_groups, per_req);
   // rows of a group, and the place of its row r
   auto rows_of = [&](int group, int &n_rows) __attribute__((always_inline)) {
     const int g = group / p.n_groups, t0 = (group - g * p.n_groups) * p.group_len;
     n_rows = min(p.group_len, p.L - t0) * p.G;
-    return (const uint8_t *)p.q + ((((size_t)b * p.gamma + g) * p.L + t0) * p.Hq + hk * p.G) * D * 2 + h * 16;
+    return (const uint8_t *)p.q + ((((size_t)b * p.gamma + g) * p.L + t0) * p.Hq + hk * p.G) * D * 2;
   };
   auto place = [&](int r) __attribute__((always_inline)) { return ((size_t)(r / p.G) * p.Hq + r % p.G) * D * 2; };
-  auto tile_scores = [&](const uint8_t *qs, f32x16 (&s)[NB]) __attribute__((always_inline)) {
-    u32x4 q[T];
+  u32x4 q[T];   // (SLOT < 32: the rows of the next groups, under way)
+  auto request_rows = [&](int group) __attribute__((always_inline)) {
+    int n_rows;
+    const uint8_t *qs = rows_of(min(group + ln / SLOT, end - 1), n_rows);
+    qs += place(min(ln % SLOT, n_rows - 1)) + h * 16;
 #pragma unroll
     for (int t = 0; t < T; ++t) q[t] = *(const u32x4 *)(qs + t * 32);
+  };
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    constexpr int kLanes = D / 4;   // lanes of a block's 4 D bytes
+#pragma unroll
+    for (int i = 0; i < kBoundBytes / 1024; ++i) {
+      const int x = i * (64 / kLanes) + lane / kLanes;             // the block among the 32
+      const int from = __shfl(blk[nb], x);
+      const int piece = (lane % kLanes) ^ (x & 15);
+      load_lds16((const uint8_t *)p.k_bounds + (((size_t)from * p.Hkv + hk) * kLanes + piece) * 16, bounds_at + i * 1024);
+    }
+    if (SLOT < 32 && nb == 0) request_rows(first);
+    wait_loads<0>();
+    const uint8_t *mine = lds + wave * kBoundBytes + ln * 4 * D;
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      lo[nb][t] = *(const u32x4 *)(mine + (((2 * t + h) ^ (ln & 15)) << 4));
+      hi[nb][t] = *(const u32x4 *)(mine + (((kPieces + 2 * t + h) ^ (ln & 15)) << 4));
+    }
+    // the next tile, and the query rows, come to the same place: this one has to be in registers first
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  auto tile_scores = [&](const u32x4 (&q)[T], f32x16 (&s)[NB]) __attribute__((always_inline)) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -108,29 +166,53 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectParams p) 
     if (h == 0 && lb < n) p.score[(((size_t)b * per_req + group) * p.Hkv + hk) * p.n_max + lb] = best;
   };
   if constexpr (SLOT == 32) {
-    for (int group = first; group < end; ++group) {
+    const int per_group = (p.group_len * p.G + 31) / 32, total = (end - first) * per_group;
+    int next_group = first, next_part = 0;   // of the tile that is requested next
+    auto request = [&](int slot) __attribute__((always_inline)) {
       int n_rows;
-      const uint8_t *base = rows_of(group, n_rows);
-      float best[NB];
+      const uint8_t *base = rows_of(next_group, n_rows);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) best[nb] = -INFINITY;
-      for (int r0 = 0; r0 < n_rows; r0 += 32) {
-        f32x16 s[NB];
-        tile_scores(base + place(min(r0 + ln, n_rows - 1)), s);  // (surplus rows repeat the last one)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int j = 0; j < 16; ++j) best[nb] = fmaxf(best[nb], s[nb][j]);
+      for (int j = 0; j < kPerWave; ++j) {
+        const int row = ((wave * kPerWave + j) * 64 + lane) / kPieces, r = min(next_part * 32 + row, n_rows - 1);  // (surplus rows repeat the last one)
+        load_lds16(base + place(r) + (((lane % kPieces) ^ (row & kMask)) << 4), lds_address(lds) + slot * kTileBytes + (wave * kPerWave + j) * 1024);
       }
+      if (++next_part == per_group) next_part = 0, next_group = min(next_group + 1, end - 1);  // (behind the last tile: others again)
+    };
+    __syncthreads();   // every wavefront has its bounds in registers
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) store(group, nb, xhalf_max(best[nb]));
+    for (int i = 0; i < kRing - 1; ++i) request(i);
+    float best[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) best[nb] = -INFINITY;
+    int group = first, part = 0;
+    for (int i = 0; i < total; ++i) {
+      wait_loads<(kRing - 2) * kPerWave>();
+      __syncthreads();   // tile i is there, and tile i - 1 has been read by all
+      request((i + kRing - 1) & (kRing - 1));
+      const uint8_t *mine = lds + (i & (kRing - 1)) * kTileBytes + ln * 2 * D;
+#pragma unroll
+      for (int t = 0; t < T; ++t) q[t] = *(const u32x4 *)(mine + (((2 * t + h) ^ (ln & kMask)) << 4));
+      f32x16 s[NB];
+      tile_scores(q, s);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) best[nb] = fmaxf(best[nb], s[nb][j]);
+      if (++part == per_group) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          store(group, nb, xhalf_max(best[nb]));
+          best[nb] = -INFINITY;
+        }
+        ++group, part = 0;
+      }
     }
+    wait_loads<0>();
   } else {
     for (int group = first; group < end; group += kShare) {
-      int n_rows;
-      const uint8_t *base = rows_of(min(group + ln / SLOT, end - 1), n_rows);
       f32x16 s[NB];
-      tile_scores(base + place(min(ln % SLOT, n_rows - 1)), s);
+      tile_scores(q, s);
+      if (group + kShare < end) request_rows(group + kShare);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -143,7 +225,7 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectParams p) 
         }
     }
   }
-  if (chunk == 0) {  // the largest magnitude among the tiles' bounds, once per request and head
+  if (chunk == 0 && tile * 32 < n) {  // the largest magnitude among the tiles' bounds, once per request and head
     uint32_t top = 0;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -238,28 +320,29 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
   id /= (uint32_t)p.Hkv;
   const int per_req = p.gamma * p.n_groups;
   const int b = (int)(id / (uint32_t)per_req), group = (int)(id % (uint32_t)per_req);
-  const int n = prefix_blocks(p, b);
   int32_t *out = p.blocks + unit * p.max_sel;
+  const float *score = p.score + unit * p.n_max;
+  const int c0 = p.keep_first;   // the first candidate
+  float item[kItems];
+  if (IN_REG && p.n_max > p.max_sel) {   // (asked for together with the prefix's length; there are n_max places)
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int i = c0 + tid + k * NT;
+      item[k] = i < p.n_max ? score[i] : 0.f;
+    }
+  }
+  const int n = prefix_blocks(p, b);
   if (n <= p.max_sel) {
     for (int i = tid; i < p.max_sel; i += NT) out[i] = i < n ? i : -1;
     if (tid == 0) p.count[unit] = n;
     return;
   }
-  const int c0 = p.keep_first, c1 = n - p.keep_last;           // candidates
+  const int c1 = n - p.keep_last;                              // candidates c0 .. c1 - 1
   const int want = p.max_sel - p.keep_first - p.keep_last;     // fewer than there are
   if (tid == 0) p.count[unit] = p.max_sel;
   for (int i = tid; i < c0; i += NT) out[i] = i;
   for (int i = tid; i < p.keep_last; i += NT) out[c0 + want + i] = c1 + i;
   if (want == 0) return;
-  const float *score = p.score + unit * p.n_max;
-  float item[kItems];
-  if constexpr (IN_REG) {
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-      const int i = c0 + tid + k * NT;
-      item[k] = i < c1 ? score[i] : -INFINITY;
-    }
-  }
   // f(place of the candidate, its score, its number among the thread's)
   auto for_each = [&](auto f) __attribute__((always_inline)) {
     if constexpr (IN_REG) {
@@ -560,14 +643,17 @@ template <int D, int SLOT, int NB>
 hipError_t launch_score(SelectParams &p, hipStream_t stream) {
   ProfileScope scope(SLOT_BLOCK_SCORE, stream);
   const int64_t groups = (int64_t)p.gamma * p.n_groups;
-  p.score_tiles = (int)((groups + 32 / SLOT - 1) / (32 / SLOT));
+  const int64_t row_tiles = (groups + 32 / SLOT - 1) / (32 / SLOT);
   p.top_blocks = 32 * NB;
   const int64_t tiles = (p.n_max + 32 * NB - 1) / (32 * NB), wgs = (tiles + 3) / 4;
   // wavefronts that go through several groups read their blocks' bounds once: as many as fill the chip about four times over
   // (2048 workgroups), the groups shared out among them
   int64_t chunks = (2048 + wgs * p.B * p.Hkv - 1) / (wgs * p.B * p.Hkv);
-  chunks = chunks < p.score_tiles ? chunks : p.score_tiles;
+  chunks = chunks < row_tiles ? chunks : row_tiles;
+  const int64_t share = (row_tiles + chunks - 1) / chunks;
+  chunks = (row_tiles + share - 1) / share;
   p.score_chunks = (int)chunks;
+  p.score_groups = (int)(share * (32 / SLOT));
   const int64_t units = chunks * p.B * p.Hkv;
   const dim3 grid((unsigned)wgs, (unsigned)(units < 65535 ? units : 65535), (unsigned)((units + 65534) / 65535));
   hipLaunchKernelGGL((block_score_kernel<D, SLOT, NB>), grid, dim3(256), 0, stream, p);

@@ -241,8 +241,8 @@ struct SelectParams {
   int max_sel, keep_first, keep_last;
   int n_max;                  // blocks of the longest prefix
   int n_tiles;                // ceil(n_max / 32)
-  // set by the launcher: tiles of 32 query rows of a request and head, the parts they are shared out in, blocks per `top`
-  int score_tiles, score_chunks, top_blocks;
+  // set by the launcher: groups that a workgroup of scores goes through, such parts of a request and head, blocks per `top`
+  int score_groups, score_chunks, top_blocks;
 };
 hipError_t launch_block_select(const SelectParams &p, hipStream_t stream);
 
