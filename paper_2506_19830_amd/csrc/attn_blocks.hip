@@ -67,12 +67,18 @@ __device__ __forceinline__ bf16x8 read_transposed(const uint8_t *p0, const uint8
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// 16 bytes per lane from memory to consecutive places in LDS, without registers in between; the wavefront that issues it waits
+// 16 bytes per lane from memory (a base the wavefront shares and an offset) to consecutive places in LDS, without registers in between; the wavefront that issues it waits
 // with wait_loads() before a barrier that lets others read.
+__device__ __forceinline__ void load_lds16(const uint8_t *base, uint32_t lane_off, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(lane_off), "s"(base), "s"(lds_addr) : "m0");
+}
 __device__ __forceinline__ void load_lds16(const uint8_t *src, uint32_t lds_addr) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds_addr) : "m0");
 }
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }  // vmcnt(0)
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
 }
@@ -190,6 +196,37 @@ __device__ __forceinline__ bool find_unit(const SparseParams &p, Unit &u, Places
   return true;
 }
 
+// Where a key of the list lies: block_at its block (keys behind the last repeat it), row_at its row in the cache.
+__device__ __forceinline__ int block_at(const SparseParams &p, const Unit &u, const Places &t, int key) {
+  return t.place[min((min(key, u.n_keys - 1) >> p.block_shift) - u.slot0, kMaxSlots - 1)];
+}
+__device__ __forceinline__ size_t row_at(const SparseParams &p, const Unit &u, int blk, int key) {
+  return (((size_t)(uint32_t)blk * (uint32_t)p.Hkv + (uint32_t)u.hk) << p.block_shift) + (min(key, u.n_keys - 1) & ((1 << p.block_shift) - 1));
+}
+// Groups of 16 keys lie in one block.  Where lanes of a wavefront share their keys' groups (attn_rows_kernel), a group's place
+// goes through scalar registers, and a lane adds its offset inside the group.
+struct KeyGroup {
+  size_t row;   // the group's first row in the cache
+  int last;     // its last key that exists (15 but at the end of the list)
+};
+// KEYS / 16 groups of tile `tile`, one of the workgroup's: lane l has the block of group l % (KEYS / 16)
+template <int KEYS>
+__device__ __forceinline__ int tile_places(const SparseParams &p, const Unit &u, const Places &t, int tile, int lane) {
+  const int key = min(tile * KEYS + (lane % (KEYS / 16)) * 16, (u.n_keys - 1) & ~15);   // (groups behind the last repeat it)
+  return t.place[min((key >> p.block_shift) - u.slot0, kMaxSlots - 1)];
+}
+template <int KEYS>
+__device__ __forceinline__ KeyGroup key_group(const SparseParams &p, const Unit &u, int places, int tile, int group) {
+  const int key = min(tile * KEYS + group * 16, (u.n_keys - 1) & ~15);
+  const int blk = __builtin_amdgcn_readlane(places, group);
+  KeyGroup g;
+  g.row = (((size_t)blk * p.Hkv + u.hk) << p.block_shift) + (key & ((1 << p.block_shift) - 1));
+  g.last = min(15, u.n_keys - 1 - key);
+  return g;
+}
+// token of the request that own key `key` of a tile is (those behind the last repeat it)
+__device__ __forceinline__ int own_row(const Unit &u, int first, int key) { return min(first + key, u.own_end - 1); }
+
 __device__ __forceinline__ size_t out_row(const SparseParams &p, const Unit &u, int r) {
   return (size_t)u.b * p.n_rows + (size_t)(u.tok0 + r / p.G) * p.Hq + u.hk * p.G + r % p.G;
 }
@@ -228,21 +265,22 @@ struct Quarter {
 template <int D>
 __device__ __forceinline__ int exp_shift(size_t row, int q) { return (int)((row * (D / 32) + q * D / 128) & 3) * 8; }
 
+// base, exps: row 0 of a group (the same for all lanes); at: the lane's row in it
 template <int FMT, int D>
-__device__ __forceinline__ void load_quarter(Quarter<FMT, D> &r, const void *base, const uint8_t *exps, size_t row, int q) {
+__device__ __forceinline__ void load_quarter(Quarter<FMT, D> &r, const uint8_t *base, const uint8_t *exps, uint32_t at, int q) {
   constexpr int N = Quarter<FMT, D>::kWords;
-  const uint8_t *src = (const uint8_t *)base + (row * 4 + q) * (N * 4);
+  const uint32_t off = at * (16 * N) + q * (N * 4);
   if constexpr (N == 2) {
-    const u32x2 x = *(const u32x2 *)src;
+    const u32x2 x = *(const u32x2 *)(base + off);
     r.w[0] = x[0], r.w[1] = x[1];
   } else {
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
-      const u32x4 x = *(const u32x4 *)(src + i * 4);
+      const u32x4 x = *(const u32x4 *)(base + off + i * 4);
       r.w[i] = x[0], r.w[i + 1] = x[1], r.w[i + 2] = x[2], r.w[i + 3] = x[3];
     }
   }
-  if constexpr (FMT != FMT_BF16) r.e = *(const uint32_t *)(exps + ((row * (D / 32) + q * D / 128) & ~(size_t)3));
+  if constexpr (FMT != FMT_BF16) r.e = *(const uint32_t *)(exps + ((at * (D / 32) + q * D / 128) & ~3u));
 }
 
 // shift: of the first group's exponent in its word
@@ -376,7 +414,7 @@ __global__ __launch_bounds__(64 * NW, (kRowsOccupancy<FMT, D, RB>)) void attn_ro
   __shared__ Places places;
   __shared__ float fold_ml[NW][RB * 16][2];
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, quarter = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, quarter = lane >> 4;
   Unit u;
   if (!find_unit<RB * 16, 32, 64 * NW>(p, u, places)) return;
   const int n_tiles = u.n_tiles;
@@ -405,20 +443,21 @@ __global__ __launch_bounds__(64 * NW, (kRowsOccupancy<FMT, D, RB>)) void attn_ro
   // the prefix: the rows of the next tile are requested before the present one is used
   const int pre_end = min(end, n_tiles);
   if (begin < pre_end) {
-    auto row_of = [&](int tile, int x) __attribute__((always_inline)) {
-      const int key = min(tile * 32 + x * 16 + n, u.n_keys - 1);
-      const int blk = places.place[(key >> p.block_shift) - u.slot0];
-      return (((size_t)blk * p.Hkv + u.hk) << p.block_shift) + (key & ((1 << p.block_shift) - 1));
-    };
     // A tile's registers are requested anew as soon as its scores and its V tile are made; the scheduling fence keeps the
     // compiler from moving the requests down to where the next tile needs them.
     Quarter<FMT, D> k[2], v[2];
+    constexpr int kRowBytes = Quarter<FMT, D>::kWords * 16;
+    // (behind the wavefront's last tile that one again: the table of places ends with the workgroup's tiles)
+    int at_places = tile_places<32>(p, u, places, begin, lane);
     auto request = [&](int tile) __attribute__((always_inline)) {
+      const int now = min(tile, pre_end - 1), pl = at_places;
+      at_places = tile_places<32>(p, u, places, min(tile + 1, pre_end - 1), lane);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const size_t row = row_of(min(tile, pre_end - 1), x);
-        load_quarter(v[x], p.v_cache, p.v_exp, row, quarter);
-        load_quarter(k[x], p.k_cache, p.k_exp, row, quarter);
+        const KeyGroup g = key_group<32>(p, u, pl, now, x);
+        const uint32_t at = (uint32_t)min(n, g.last);
+        load_quarter(v[x], (const uint8_t *)p.v_cache + g.row * kRowBytes, p.v_exp + g.row * (D / 32), at, quarter);
+        load_quarter(k[x], (const uint8_t *)p.k_cache + g.row * kRowBytes, p.k_exp + g.row * (D / 32), at, quarter);
       }
     };
     // (a block's rows begin at a multiple of 16, so the key says where in its word an exponent is)
@@ -455,12 +494,12 @@ __global__ __launch_bounds__(64 * NW, (kRowsOccupancy<FMT, D, RB>)) void attn_ro
     f32x4 s[RB][2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const size_t row = ((size_t)u.b * p.gamma * p.L + min(first + x * 16 + n, u.own_end - 1)) * p.Hkv + u.hk;
+      const size_t row = (((size_t)u.b * p.gamma * p.L + own_row(u, first, x * 16 + n)) * p.Hkv + u.hk) * D * 2;
       Quarter<FMT_BF16, D> r;
-      load_quarter(r, p.v_branch, nullptr, row, quarter);
+      load_quarter(r, (const uint8_t *)p.v_branch + row, nullptr, 0, quarter);
       stage_rows(lds, vt_write, x, r, 0);
       wave_order();   // (one half row in registers at a time)
-      load_quarter(r, p.k_branch, nullptr, row, quarter);
+      load_quarter(r, (const uint8_t *)p.k_branch + row, nullptr, 0, quarter);
       scores_rows(s, x, r, 0, st);
       wave_order();
     }
@@ -535,13 +574,23 @@ struct Stage {
   static constexpr int kGroups = kChunks < 4 ? 1 : kChunks / 4;                   // wavefront loads per 16 keys
   static constexpr int kTensor = FMT == FMT_BF16 ? KEYS * kChunks / 64 : KEYS / 16 * kGroups;   // of K, and of V
   static constexpr int kLoads = (2 * kTensor + NW - 1) / NW;
+  // a wavefront's loads of V are those of K a tile earlier: their rows need not be found again
+  static constexpr bool kAgain = kTensor % NW == 0;
   u32x4 w[FMT == FMT_BF16 ? 1 : kLoads];
   uint32_t e[FMT == FMT_BF16 ? 1 : kLoads];
 };
 
+// The key of a tile that a lane fetches (a piece of) by load `at` of a tensor.
+template <int FMT, int D, int KEYS, int NW>
+__device__ __forceinline__ int stage_key(int at, int lane) {
+  using S = Stage<FMT, D, KEYS, NW>;
+  return FMT == FMT_BF16 ? (at * 64 + lane) / S::kChunks : at / S::kGroups * 16 + (lane & 15);
+}
+
+// row_of(i): the row for load i; kt, vt: the tiles' places in LDS (bf16)
 template <int FMT, int D, int KEYS, int NW, typename F>
-__device__ __forceinline__ void stage_load(Stage<FMT, D, KEYS, NW> &g, const uint8_t *lds, const void *kb, const void *vb, const uint8_t *kx,
-                                           const uint8_t *vx, F row_of) {
+__device__ __forceinline__ void stage_load(Stage<FMT, D, KEYS, NW> &g, const uint8_t *kt, const uint8_t *vt, const void *kb, const void *vb,
+                                           const uint8_t *kx, const uint8_t *vx, F row_of) {
   using S = Stage<FMT, D, KEYS, NW>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
@@ -549,23 +598,22 @@ __device__ __forceinline__ void stage_load(Stage<FMT, D, KEYS, NW> &g, const uin
     const int load = wave + i * NW, which = load >= S::kTensor ? 1 : 0, at = load - which * S::kTensor;
     if (load >= 2 * S::kTensor) continue;
     const uint8_t *base = (const uint8_t *)(which ? vb : kb);
+    const size_t row = row_of(i);
     if constexpr (FMT == FMT_BF16) {
-      constexpr int kRows = 64 / S::kChunks;
-      const int first = at * kRows, key = first + lane / S::kChunks;
-      load_lds16(base + (row_of(key) * S::kChunks + ((lane % S::kChunks) ^ swizzle<D>(key))) * 16,
-                 lds_address(lds) + (which * KEYS + first) * D * 2);
+      const int chunk = (lane % S::kChunks) ^ swizzle<D>(stage_key<FMT, D, KEYS, NW>(at, lane));
+      load_lds16(base + (row * S::kChunks + chunk) * 16, lds_address(which ? vt : kt) + at * 1024);
     } else {
-      const int key = at / S::kGroups * 16 + (lane & 15), chunk = min((lane >> 4) + 4 * (at % S::kGroups), S::kChunks - 1);
-      const size_t row = row_of(key);
+      const int chunk = min((lane >> 4) + 4 * (at % S::kGroups), S::kChunks - 1);
       g.w[i] = *(const u32x4 *)(base + (row * S::kChunks + chunk) * 16);
       g.e[i] = *(const uint32_t *)((which ? vx : kx) + ((row * (D / 32) + chunk * S::kElems / 32) & ~(size_t)3));
     }
   }
 }
 
-// Before the barrier behind which the tile is read.  last: the tile's last key that exists (those behind it repeat it).
+// Before the barrier behind which the tiles are read.  k_last, v_last: the last key of each that exists (those behind it repeat
+// it).
 template <int FMT, int D, int KEYS, int NW>
-__device__ __forceinline__ void stage_store(const Stage<FMT, D, KEYS, NW> &g, uint8_t *lds, int last) {
+__device__ __forceinline__ void stage_store(const Stage<FMT, D, KEYS, NW> &g, uint8_t *kt, uint8_t *vt, int k_last, int v_last) {
   using S = Stage<FMT, D, KEYS, NW>;
   if constexpr (FMT == FMT_BF16) {
     wait_loads();
@@ -580,9 +628,9 @@ __device__ __forceinline__ void stage_store(const Stage<FMT, D, KEYS, NW> &g, ui
       if (S::kChunks < 4 && chunk >= S::kChunks) continue;   // (a D = 64 row of fp4 has two chunks)
       const uint32_t w[4] = {g.w[i][0], g.w[i][1], g.w[i][2], g.w[i][3]};
       // (a block's rows begin at a multiple of 16, so the key says where in its word an exponent is)
-      const uint32_t e = (g.e[i] >> (((min(key, last) * (D / 32) + chunk * S::kElems / 32) & 3) * 8)) & 0xffu;
+      const uint32_t e = (g.e[i] >> (((min(key, which ? v_last : k_last) * (D / 32) + chunk * S::kElems / 32) & 3) * 8)) & 0xffu;
       const int row = key * D * 2 + (((chunk * kPieces) ^ swizzle<D>(key)) << 4);
-      uint8_t *to = lds + which * KEYS * D * 2;
+      uint8_t *to = which ? vt : kt;
 #pragma unroll
       for (int t = 0; t < kPieces; ++t) *(u32x4 *)(to + (row ^ (t << 4))) = widen8<FMT>(w + t * kWords8<FMT>, exp_scale(e));
     }
@@ -597,12 +645,9 @@ struct TileRows {
   int tok, start;
 };
 
-// A wavefront's NB blocks of 32 keys of a tile in LDS: scores, probabilities, product with V.  kt, vt: offsets of the lane's K
-// and V operands in LDS; first: the first key.
-template <int D, int NB, int MASK>
-__device__ __forceinline__ void attend_tile(TileRows<D> &st, const uint8_t *lds, int kt, int vt, float scale_log2, int first, int limit, int lane) {
-  const int h = lane >> 5;
-  f32x16 s[NB];
+// A wavefront's NB blocks of 32 keys of a tile.  kt, vt: offsets of the lane's K and V operands in LDS.
+template <int D, int NB>
+__device__ __forceinline__ void tile_scores(f32x16 (&s)[NB], const TileRows<D> &st, const uint8_t *lds, int kt) {
 #pragma unroll
   for (int kb = 0; kb < NB; ++kb) {
 #pragma unroll
@@ -613,6 +658,12 @@ __device__ __forceinline__ void attend_tile(TileRows<D> &st, const uint8_t *lds,
       s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, st.q[t], s[kb], 0, 0, 0);
     }
   }
+}
+
+// Masks, and the running maximum (raised only when a tile exceeds it by kRaise: until then probabilities may reach 2^kRaise).
+// first: the first key; keys from `limit` on do not exist (TILE_TAIL).
+template <int D, int NB, int MASK>
+__device__ __forceinline__ void tile_max(f32x16 (&s)[NB], TileRows<D> &st, float scale_log2, int first, int limit, int h) {
   float top = -INFINITY;
 #pragma unroll
   for (int kb = 0; kb < NB; ++kb)
@@ -638,43 +689,106 @@ __device__ __forceinline__ void attend_tile(TileRows<D> &st, const uint8_t *lds,
       for (int j = 0; j < 16; ++j) st.o[db][j] *= alpha;
   }
   st.m = m;
-  const float base = m == -INFINITY ? 0.f : m;  // no key seen yet: every score is -inf
+}
+
+// Probabilities of a block of 32 keys and their sum.
+template <int D>
+__device__ __forceinline__ void tile_probs(bf16x8 (&pf)[2], const f32x16 &s, TileRows<D> &st, float scale_log2) {
+  const float base = st.m == -INFINITY ? 0.f : st.m;  // no key seen yet: every score is -inf
   float sum = 0.f;
 #pragma unroll
-  for (int kb = 0; kb < NB; ++kb)
+  for (int c = 0; c < 2; ++c) {
+    u32x4 pw;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      u32x4 pw;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][8 * c + 2 * x], scale_log2, -base));
-        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][8 * c + 2 * x + 1], scale_log2, -base));
-        sum += p0 + p1;
-        pw[x] = pack_bf16(p0, p1);
-      }
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
-      // V^T operands: lane (d, h) takes keys 16 c + 4 h + 0..3 and 8 more, the order of the probabilities
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        const uint8_t *at = lds + (kb * 32 + 16 * c) * D * 2;
-        const bf16x8 vf = read_transposed(at + (vt ^ (db << 6)), at + (vt ^ (db << 6) ^ 32) + 8 * D * 2);
-        st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, st.o[db], 0, 0, 0);
-      }
+    for (int x = 0; x < 4; ++x) {
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * c + 2 * x], scale_log2, -base));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * c + 2 * x + 1], scale_log2, -base));
+      sum += p0 + p1;
+      pw[x] = pack_bf16(p0, p1);
     }
+    pf[c] = __builtin_bit_cast(bf16x8, pw);
+  }
   st.l += sum;
+}
+
+// V^T operands: lane (d, h) takes keys 16 c + 4 h + 0..3 and 8 more, the order of the probabilities.
+template <int D>
+__device__ __forceinline__ void tile_values(TileRows<D> &st, const bf16x8 (&pf)[2], const uint8_t *lds, int vt) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const uint8_t *at = lds + 16 * c * D * 2;
+      const bf16x8 vf = read_transposed(at + (vt ^ (db << 6)), at + (vt ^ (db << 6) ^ 32) + 8 * D * 2);
+      st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[c], st.o[db], 0, 0, 0);
+    }
+}
+
+// 2^x at this place of the instruction stream: the compiler would gather the exponentials of a step behind its matrix
+// instructions.  (The wait state lies between a transcendental instruction and what reads its result.)
+__device__ __forceinline__ float exp2_here(float x) {
+  float y;
+  asm volatile("v_exp_f32 %0, %1\n\ts_nop 0" : "=v"(y) : "v"(x));
+  return y;
+}
+
+// One block of 32 keys' probabilities and product with V, and the scores of the block that comes next: the matrix cores form
+// these while the exponentials run.  The order is written out -- a matrix instruction, the vector work of two probabilities, the
+// reads of operands that are needed later -- and fenced, or the compiler would put each kind of work in a row of its own.
+template <int D>
+__device__ __forceinline__ void tile_step(f32x16 &next, const f32x16 &s, TileRows<D> &st, const uint8_t *k_lds, int kt, const uint8_t *v_lds, int vt,
+                                          float scale_log2) {
+  constexpr int T = D / 16, kAhead = 4, kEach = 16 / T;  // matrix instructions; K operands under way; probabilities between two of them
+  static_assert(T >= kAhead && 16 % T == 0, "head dimensions 64, 128 and 256");
+  const float base = st.m == -INFINITY ? 0.f : st.m;  // no key seen yet: every score is -inf
+  auto read_k = [&](int t) __attribute__((always_inline)) { return *(const bf16x8 *)(k_lds + (kt ^ (t << 5))); };
+  bf16x8 kf[T], vf[T];
+  float pr[16], sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < kAhead; ++t) kf[t] = read_k(t);
+#pragma unroll
+  for (int j = 0; j < 16; ++j) next[j] = 0.f;
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    if (t + kAhead < T) kf[t + kAhead] = read_k(t + kAhead);
+    // V operand t: keys 16 c .., elements 32 db ..
+    const int c = t / (D / 32), db = t % (D / 32);
+    const uint8_t *at = v_lds + 16 * c * D * 2;
+    vf[t] = read_transposed(at + (vt ^ (db << 6)), at + (vt ^ (db << 6) ^ 32) + 8 * D * 2);
+    next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t], st.q[t], next, 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = t * kEach; j < (t + 1) * kEach; ++j) pr[j] = exp2_here(__builtin_fmaf(s[j], scale_log2, -base));
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int j = 0; j < 16; ++j) sum += pr[j];
+  st.l += sum;
+  bf16x8 pf[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    u32x4 pw;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) pw[x] = pack_bf16(pr[8 * c + 2 * x], pr[8 * c + 2 * x + 1]);
+    pf[c] = __builtin_bit_cast(bf16x8, pw);
+  }
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+    st.o[t % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t], pf[t / (D / 32)], st.o[t % (D / 32)], 0, 0, 0);
 }
 
 // RW wavefronts side by side along the rows, KS along the keys of a tile.
 template <int FMT, int D, int RW, int KS>
-__global__ __launch_bounds__(64 * RW * KS, 2) void attn_tile_kernel(const SparseParams p) {
+__global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void attn_tile_kernel(const SparseParams p) {
   constexpr int KEYS = D == 256 ? 32 : 64, NB = KEYS / 32 / KS, NW = RW * KS;
-  static_assert(NB >= 1, "every wavefront has keys of a tile");
+  static_assert(NB == 1, "every wavefront has 32 keys of a tile");
   constexpr int kTileBytes = KEYS * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kTileBytes];  // two buffers of a K and a V tile
   __shared__ Places places;
   __shared__ float fold_ml[RW * 32][2];
   static_assert(KS == 1 || RW * (D / 32) * 16 * 64 * 4 <= 4 * kTileBytes, "the accumulators of the upper keys fit");
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ln = lane & 31, h = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ln = lane & 31, h = lane >> 5;
   const int row_wave = wave % RW, key_wave = wave / RW;
   Unit u;
   if (!find_unit<RW * 32, KEYS, 64 * NW>(p, u, places)) return;
@@ -693,50 +807,105 @@ __global__ __launch_bounds__(64 * RW * KS, 2) void attn_tile_kernel(const Sparse
 #pragma unroll
       for (int j = 0; j < 16; ++j) st.o[db][j] = 0.f;
   }
-  const bool any_row = u.r0 + row_wave * 32 < u.n_rows;  // (a wavefront without rows only helps to stage)
   // the lane's operands in a buffer (a row's pieces are permuted inside the row, whose size is a power of two: XOR)
   const int i = lane & 15, read_key = 4 * h + (i >> 2), my_keys = key_wave * NB * 32;
   const int kt = (my_keys + ln) * D * 2 + ((h ^ swizzle<D>(ln)) << 4);
-  const int vt = kTileBytes + (my_keys + read_key) * D * 2 +
-                 (((2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ swizzle<D>(read_key)) << 4) + (i & 1) * 8;
+  const int vt = (my_keys + read_key) * D * 2 + (((2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ swizzle<D>(read_key)) << 4) + (i & 1) * 8;
+  uint8_t *k_lds = lds, *v_lds = lds + 2 * kTileBytes;  // two K tiles, two V tiles
   __syncthreads();
 
+  // The prefix.  While the probabilities and the values of one tile are worked on, the matrix cores already form the next one's
+  // scores: a step needs the V tile of its own and the K tile of the next, and requests the K tile behind that and the next V.
   if (begin < pre_end) {
     Stage<FMT, D, KEYS, NW> g;
-    auto load = [&](int tile, const uint8_t *to) __attribute__((always_inline)) {
-      stage_load(g, to, p.k_cache, p.v_cache, p.k_exp, p.v_exp, [&](int in_tile) __attribute__((always_inline)) {
-        const int key = min(tile * KEYS + in_tile, u.n_keys - 1);
-        const int blk = places.place[(key >> p.block_shift) - u.slot0];
-        return (((size_t)blk * p.Hkv + u.hk) << p.block_shift) + (key & ((1 << p.block_shift) - 1));
-      });
+    using S = Stage<FMT, D, KEYS, NW>;
+    // Tiles behind the last one repeat it.  (v_tile is the last request's k_tile.)  The table of places is read a tile ahead.
+    constexpr int kRows = S::kAgain ? S::kTensor / NW : S::kLoads;
+    size_t row[kRows], row_before[kRows];
+    int blk[kRows];
+    auto key_of = [&](int i, int k_tile, int v_tile) __attribute__((always_inline)) {
+      const int load = wave + i * NW, which = load >= S::kTensor ? 1 : 0;
+      return min(which ? v_tile : k_tile, pre_end - 1) * KEYS + stage_key<FMT, D, KEYS, NW>(load - which * S::kTensor, lane);
     };
-    load(begin, lds);
-    stage_store(g, lds, u.n_keys - 1 - begin * KEYS);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) blk[i] = block_at(p, u, places, key_of(i, begin, begin)), row[i] = 0;
+    auto request = [&](int k_tile, int v_tile) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        row_before[i] = row[i], row[i] = row_at(p, u, blk[i], key_of(i, k_tile, v_tile));
+        blk[i] = block_at(p, u, places, key_of(i, k_tile + 1, k_tile));
+      }
+      stage_load(g, k_lds + (k_tile & 1) * kTileBytes, v_lds + (v_tile & 1) * kTileBytes, p.k_cache, p.v_cache, p.k_exp, p.v_exp,
+                 [&](int i) __attribute__((always_inline)) { return i < kRows ? row[i] : row_before[i % kRows]; });
+    };
+    auto deliver = [&](int k_tile, int v_tile) __attribute__((always_inline)) {
+      stage_store(g, k_lds + (k_tile & 1) * kTileBytes, v_lds + (v_tile & 1) * kTileBytes,
+                  u.n_keys - 1 - min(k_tile, pre_end - 1) * KEYS, u.n_keys - 1 - min(v_tile, pre_end - 1) * KEYS);
+    };
+    request(begin, begin);   // (of V nothing that is used)
+    deliver(begin, begin);
+    request(begin + 1, begin);
     __syncthreads();
+    f32x16 s[NB];
+    tile_scores(s, st, k_lds + (begin & 1) * kTileBytes, kt);
+    if ((begin + 1) * KEYS <= u.n_keys)
+      tile_max<D, NB, TILE_FULL>(s, st, p.scale_log2, begin * KEYS + my_keys, u.n_keys, h);
+    else
+      tile_max<D, NB, TILE_TAIL>(s, st, p.scale_log2, begin * KEYS + my_keys, u.n_keys, h);
+    deliver(begin + 1, begin);
+    __syncthreads();
+    auto weigh = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb) {
+        bf16x8 pf[2];
+        tile_probs(pf, s[kb], st, p.scale_log2);
+        tile_values(st, pf, v_lds + (tile & 1) * kTileBytes + kb * 32 * D * 2, vt);
+      }
+    };
     const int full_end = min(pre_end, u.n_keys / KEYS);   // (only the list's last tile can be a partial one)
-    int at = 0;
-    for (int tile = begin; tile < full_end; ++tile, at ^= 2 * kTileBytes) {
-      uint8_t *other = lds + (at ^ (2 * kTileBytes));
-      if (tile + 1 < pre_end) load(tile + 1, other);
-      if (any_row) attend_tile<D, NB, TILE_FULL>(st, lds + at, kt, vt, p.scale_log2, tile * KEYS + my_keys, u.n_keys, lane);
-      if (tile + 1 < pre_end) stage_store(g, other, u.n_keys - 1 - (tile + 1) * KEYS);
+    int tile = begin;
+    for (; tile + 1 < full_end; ++tile) {
+      request(tile + 2, tile + 1);
+      f32x16 next[1];
+      tile_step<D>(next[0], s[0], st, k_lds + ((tile + 1) & 1) * kTileBytes, kt, v_lds + (tile & 1) * kTileBytes, vt, p.scale_log2);
+      tile_max<D, 1, TILE_FULL>(next, st, p.scale_log2, (tile + 1) * KEYS + my_keys, u.n_keys, h);
+      s[0] = next[0];
+      deliver(tile + 2, tile + 1);
       __syncthreads();
     }
-    if (full_end < pre_end) {
-      if (any_row) attend_tile<D, NB, TILE_TAIL>(st, lds + at, kt, vt, p.scale_log2, full_end * KEYS + my_keys, u.n_keys, lane);
+    if (tile + 1 < pre_end) {
+      request(tile + 2, tile + 1);
+      weigh(tile);
+      tile_scores(s, st, k_lds + ((tile + 1) & 1) * kTileBytes, kt);
+      tile_max<D, NB, TILE_TAIL>(s, st, p.scale_log2, (tile + 1) * KEYS + my_keys, u.n_keys, h);
+      deliver(tile + 2, tile + 1);
       __syncthreads();
     }
+    weigh(pre_end - 1);
+    __syncthreads();
   }
   // the branches' own tokens
   for (int tile = max(begin, n_tiles); tile < end; ++tile) {
     const int first = u.own0 + (tile - n_tiles) * KEYS;
-    Stage<FMT_BF16, D, KEYS, NW> g;
-    stage_load(g, lds, p.k_branch, p.v_branch, nullptr, nullptr, [&](int in_tile) __attribute__((always_inline)) {
-      return ((size_t)u.b * p.gamma * p.L + min(first + in_tile, u.own_end - 1)) * p.Hkv + u.hk;
-    });
-    stage_store(g, lds, 0);
+    constexpr int kPieces = D / 8;
+    for (int load = __builtin_amdgcn_readfirstlane(wave); load < 2 * KEYS * kPieces / 64; load += NW) {
+      const int which = load >= KEYS * kPieces / 64 ? 1 : 0, row0 = (load - which * (KEYS * kPieces / 64)) * (64 / kPieces);
+      const int key = row0 + lane / kPieces;
+      const size_t row = ((size_t)u.b * p.gamma * p.L + own_row(u, first, key)) * p.Hkv + u.hk;
+      const uint8_t *src = (const uint8_t *)(which ? p.v_branch : p.k_branch) + (row * kPieces + ((lane % kPieces) ^ swizzle<D>(key))) * 16;
+      load_lds16(src, lds_address(which ? v_lds : k_lds) + row0 * D * 2);
+    }
+    wait_loads();
     __syncthreads();
-    if (any_row) attend_tile<D, NB, TILE_OWN>(st, lds, kt, vt, p.scale_log2, first + my_keys, u.own_end, lane);
+    f32x16 s[NB];
+    tile_scores(s, st, k_lds, kt);
+    tile_max<D, NB, TILE_OWN>(s, st, p.scale_log2, first + my_keys, u.own_end, h);
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+      bf16x8 pf[2];
+      tile_probs(pf, s[kb], st, p.scale_log2);
+      tile_values(st, pf, v_lds + kb * 32 * D * 2, vt);
+    }
     __syncthreads();
   }
 

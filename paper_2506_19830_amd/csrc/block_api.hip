@@ -175,7 +175,7 @@ la_status plan_sparse(const la_attn_desc *d, const la_select_desc *s, const int3
       const int64_t rounds = (units * n + cus - 1) / cus;
       const double even_us = (double)rounds * ((double)most / (double)n * busy + start);
       const bool even = most_keys * d->num_requests == all_keys;
-      double us = even ? even_us : all_us + 0.5 * longest_us;
+      double us = even ? even_us : all_us + 0.25 * longest_us;
       us = (us > longest_us ? us : longest_us) + merge_us;
       if (best < 0.0 || us < best) {
         best = us;
