@@ -13,10 +13,10 @@
 // scores, maxima, sums and accumulators are fp32.
 //
 // Two kernels.  With up to 32 rows to a group (attn_rows_kernel) the work is a stream of keys that few rows look at: every
-// wavefront takes tiles of 32 keys of its own for all rows, K going from memory into matrix operands through registers
-// alone, and the wavefronts are folded at the end.  With more rows (attn_tile_kernel) four wavefronts of 32 rows each share
-// tiles of 64 keys that they widen into LDS together (up to 64 rows: two by two, each pair with half of a tile's keys).  Workgroups that share a group's keys leave partial results that the
-// merge of long splits joins.
+// wavefront takes tiles of 32 keys of its own for all rows, and the wavefronts are folded at the end.  With more rows
+// (attn_tile_kernel) two, three or four pairs of wavefronts with 32 rows each, one for either half of the keys, share tiles
+// of 64 keys that they widen into LDS together (head dimension 256: four wavefronts and 32 keys).  Workgroups that share a
+// group's keys leave partial results that the merge of long splits joins.
 #include "attn_common.hpp"
 
 namespace la {
@@ -59,6 +59,13 @@ __device__ __forceinline__ int swizzle(int key) {
   return D == 64 ? (((key >> 1) & 1) << 2) | ((key >> 2) & 3) : ((key & 3) << 2) | ((key >> 2) & 3);
 }
 
+// The same where a store covers whole rows one after the other and a transposing read 16 keys x 32 bytes (attn_rows_kernel): the
+// pieces of a chunk that a lane widens come one per store, so neighbouring rows differ in the lowest bits.
+template <int D>
+__device__ __forceinline__ int swizzle_rows(int key) {
+  return D == 64 ? ((key >> 1) & 3) | (((key >> 3) & 1) << 2) : key & 15;
+}
+
 // Two transposing reads side by side: four keys of one element from each place.  (Joined as vectors of 16-bit numbers: joined
 // as 32-bit words, the compiler copied every pair of registers once more.)
 __device__ __forceinline__ bf16x8 read_transposed(const uint8_t *p0, const uint8_t *p1) {
@@ -67,8 +74,8 @@ __device__ __forceinline__ bf16x8 read_transposed(const uint8_t *p0, const uint8
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// 16 bytes per lane from memory (a base the wavefront shares and an offset) to consecutive places in LDS, without registers in between; the wavefront that issues it waits
-// with wait_loads() before a barrier that lets others read.
+// 16 bytes per lane from memory (a base the wavefront shares and an offset, or an address) to consecutive places in LDS, without
+// registers in between; the wavefront that issues it waits with wait_loads() before it reads, or a barrier lets others read.
 __device__ __forceinline__ void load_lds16(const uint8_t *base, uint32_t lane_off, uint32_t lds_addr) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(lane_off), "s"(base), "s"(lds_addr) : "m0");
 }
@@ -77,6 +84,12 @@ __device__ __forceinline__ void load_lds16(const uint8_t *src, uint32_t lds_addr
 }
 __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+// Before loads are sent to a place in LDS that was read.
+__device__ __forceinline__ void wait_reads() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
@@ -400,6 +413,80 @@ __device__ __forceinline__ void stage_rows(uint8_t *lds, int vt_write, int u, co
   for (int t = 0; t < D / 32; ++t) *(u32x4 *)(lds + (vt_write ^ (t << 4)) + u * 16 * D * 2) = widen<FMT, D>(v, t, shift);
 }
 
+// A tile of 32 keys on its way to one wavefront.  The tag look-ups of the cache are what such a stream can be bound by: a load
+// whose neighbouring lanes read different rows takes one for every lane, one whose lanes read whole rows one for 64 bytes or
+// more.  V comes in whole rows, through registers, and goes to LDS as bf16.  K wants a row for every lane: quantised, a lane's
+// quarter of a row is one or two loads, which is cheaper than a way through LDS (32 requests x 32 blocks, fp4: 17.2 us, through
+// LDS 20.9; groups of one token and 6 rows, fp8: 26.4 us and 28.6; V and K both a row for every lane: 17.1 and 36.6); as
+// bf16 it is four, and K goes through LDS as stored (48 requests: 79 us and 105).  There the pieces of a row lie permuted: piece
+// c of key k at c ^ key_mix(k), so that one piece of 16 keys misses no bank.
+template <int FMT, int D>
+struct Stream {
+  static constexpr int kRowBytes = FMT == FMT_BF16 ? 2 * D : FMT == FMT_MX8 ? D : D / 2;
+  static constexpr int kChunks = kRowBytes / 16, kElems = D / kChunks;   // of a row; elements of a chunk
+  static constexpr int kLoads = kChunks / 2, kRows = 64 / kChunks;        // of a tensor's tile; rows of a load
+  static constexpr bool kStaged = FMT == FMT_BF16;                        // K goes through LDS
+  static constexpr int kKeyBytes = kStaged ? 32 * kRowBytes : 0;
+  u32x4 v[kLoads];
+  uint32_t ve[kLoads];
+  Quarter<FMT, D> k[2];
+  static __device__ __forceinline__ int key_mix(int key) { return kChunks < 16 ? (key * kChunks / 16) & (kChunks - 1) : key & 15; }
+};
+
+// k_lds: the wavefront's place for K.  group_of(x): keys 16 x .. of the tile.
+template <int FMT, int D, typename F>
+__device__ __forceinline__ void stream_load(Stream<FMT, D> &g, uint32_t k_lds, const SparseParams &p, int lane, F group_of) {
+  using S = Stream<FMT, D>;
+  const KeyGroup kg[2] = {group_of(0), group_of(1)};
+#pragma unroll
+  for (int i = 0; i < S::kLoads; ++i) {
+    const int key = i * S::kRows + lane / S::kChunks, chunk = lane % S::kChunks;
+    // (where a row has two chunks a load is all 32 keys, otherwise its keys are of one group)
+    const bool upper = S::kRows > 16 ? lane >= 32 : i * S::kRows >= 16;
+    const size_t first = upper ? kg[1].row : kg[0].row;
+    const uint32_t at = (uint32_t)min(key & 15, upper ? kg[1].last : kg[0].last), off = at * S::kRowBytes;
+    if constexpr (S::kStaged) load_lds16((const uint8_t *)p.k_cache + first * S::kRowBytes, off + (chunk ^ S::key_mix(key)) * 16, k_lds + i * 1024);
+    g.v[i] = *(const u32x4 *)((const uint8_t *)p.v_cache + first * S::kRowBytes + off + chunk * 16);
+    if constexpr (FMT != FMT_BF16) g.ve[i] = *(const uint32_t *)(p.v_exp + first * (D / 32) + ((at * (D / 32) + chunk * S::kElems / 32) & ~3u));
+  }
+  if constexpr (!S::kStaged) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      load_quarter(g.k[x], (const uint8_t *)p.k_cache + kg[x].row * S::kRowBytes, p.k_exp + kg[x].row * (D / 32), (uint32_t)min(lane & 15, kg[x].last),
+                   lane >> 4);
+  }
+}
+
+// V into its place.  last: the tile's last key that exists.  (A block's rows begin at a multiple of 16, so the key says where in
+// its word an exponent is.)
+template <int FMT, int D>
+__device__ __forceinline__ void stream_values(const Stream<FMT, D> &g, uint8_t *v_lds, int last, int lane) {
+  using S = Stream<FMT, D>;
+  constexpr int kPieces = S::kElems / 8;
+#pragma unroll
+  for (int i = 0; i < S::kLoads; ++i) {
+    const int key = i * S::kRows + lane / S::kChunks, chunk = lane % S::kChunks;
+    const int row = key * D * 2 + (((chunk * kPieces) ^ swizzle_rows<D>(key)) << 4);
+    const uint32_t w[4] = {g.v[i][0], g.v[i][1], g.v[i][2], g.v[i][3]};
+    float scale = 0.f;
+    if constexpr (FMT != FMT_BF16) scale = exp_scale((g.ve[i] >> (((min(key, last) * (D / 32) + chunk * S::kElems / 32) & 3) * 8)) & 0xffu);
+#pragma unroll
+    for (int t = 0; t < kPieces; ++t) *(u32x4 *)(v_lds + (row ^ (t << 4))) = widen8<FMT>(w + t * kWords8<FMT>, scale);
+  }
+}
+
+// The lane's quarter of key n of group x, out of LDS.
+template <int D>
+__device__ __forceinline__ void staged_quarter(Quarter<FMT_BF16, D> &r, const uint8_t *k_lds, int x, int lane) {
+  using S = Stream<FMT_BF16, D>;
+  const int key = x * 16 + (lane & 15), first = (lane >> 4) * (S::kChunks / 4);
+#pragma unroll
+  for (int i = 0; i < S::kChunks / 4; ++i) {
+    const u32x4 w = *(const u32x4 *)(k_lds + key * S::kRowBytes + (((first + i) ^ S::key_mix(key)) << 4));
+    r.w[4 * i] = w[0], r.w[4 * i + 1] = w[1], r.w[4 * i + 2] = w[2], r.w[4 * i + 3] = w[3];
+  }
+}
+
 // Wavefronts of a SIMD that the registers are allotted for: a wavefront alone issues a vector instruction about every other
 // time it could, so as many as the accumulators leave room for.
 template <int FMT, int D, int RB>
@@ -408,8 +495,9 @@ constexpr int kRowsOccupancy = D == 256 ? (RB == 1 ? 2 : 1) : RB == 2 ? 2 : D ==
 template <int FMT, int D, int RB, int NW>
 __global__ __launch_bounds__(64 * NW, (kRowsOccupancy<FMT, D, RB>)) void attn_rows_kernel(const SparseParams p) {
   constexpr int kTileBytes = 32 * D * 2;            // V tile of a wavefront
+  constexpr int kKeyBytes = Stream<FMT, D>::kKeyBytes;   // its K tile, as stored
   constexpr int kOne = RB * (D / 16) * 4 * 64;      // floats of one wavefront's accumulators
-  constexpr int kBytes = NW * kTileBytes > NW / 2 * kOne * 4 ? NW * kTileBytes : NW / 2 * kOne * 4;
+  constexpr int kTiles = NW * (kTileBytes + kKeyBytes), kBytes = kTiles > NW / 2 * kOne * 4 ? kTiles : NW / 2 * kOne * 4;
   __shared__ __attribute__((aligned(16))) uint8_t lds[kBytes];
   __shared__ Places places;
   __shared__ float fold_ml[NW][RB * 16][2];
@@ -437,44 +525,38 @@ __global__ __launch_bounds__(64 * NW, (kRowsOccupancy<FMT, D, RB>)) void attn_ro
   __syncthreads();
 
   // offsets into LDS (a row's pieces are permuted inside the row, whose size is a power of two: pieces are reached by XOR)
-  const int vt_write = wave * kTileBytes + n * D * 2 + (((quarter * (D / 32)) ^ swizzle<D>(n)) << 4);
+  const int vt_write = wave * kTileBytes + n * D * 2 + (((quarter * (D / 32)) ^ swizzle_rows<D>(n)) << 4);
   const int read_key = 4 * quarter + (n >> 2);
-  const int vt_read = wave * kTileBytes + read_key * D * 2 + ((((n & 3) >> 1) ^ swizzle<D>(read_key)) << 4) + (n & 1) * 8;
+  const int vt_read = wave * kTileBytes + read_key * D * 2 + ((((n & 3) >> 1) ^ swizzle_rows<D>(read_key)) << 4) + (n & 1) * 8;
   // the prefix: the rows of the next tile are requested before the present one is used
   const int pre_end = min(end, n_tiles);
   if (begin < pre_end) {
-    // A tile's registers are requested anew as soon as its scores and its V tile are made; the scheduling fence keeps the
+    // A tile is requested anew as soon as the scores and the V tile of the one before are made; the scheduling fence keeps the
     // compiler from moving the requests down to where the next tile needs them.
-    Quarter<FMT, D> k[2], v[2];
-    constexpr int kRowBytes = Quarter<FMT, D>::kWords * 16;
-    // (behind the wavefront's last tile that one again: the table of places ends with the workgroup's tiles)
+    Stream<FMT, D> g;
+    uint8_t *k_lds = lds + NW * kTileBytes + wave * kKeyBytes;
     int at_places = tile_places<32>(p, u, places, begin, lane);
     auto request = [&](int tile) __attribute__((always_inline)) {
-      const int now = min(tile, pre_end - 1), pl = at_places;
-      at_places = tile_places<32>(p, u, places, min(tile + 1, pre_end - 1), lane);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const KeyGroup g = key_group<32>(p, u, pl, now, x);
-        const uint32_t at = (uint32_t)min(n, g.last);
-        load_quarter(v[x], (const uint8_t *)p.v_cache + g.row * kRowBytes, p.v_exp + g.row * (D / 32), at, quarter);
-        load_quarter(k[x], (const uint8_t *)p.k_cache + g.row * kRowBytes, p.k_exp + g.row * (D / 32), at, quarter);
-      }
+      const int pl = at_places;
+      at_places = tile_places<32>(p, u, places, min(tile + 1, pre_end - 1), lane);   // (the table ends with the workgroup's tiles)
+      stream_load(g, lds_address(k_lds), p, lane, [&](int x) __attribute__((always_inline)) { return key_group<32>(p, u, pl, tile, x); });
     };
-    // (a block's rows begin at a multiple of 16, so the key says where in its word an exponent is)
     auto consume = [&](f32x4 (&s)[RB][2], int last) __attribute__((always_inline)) {
+      if constexpr (Stream<FMT, D>::kStaged) wait_loads();
+      stream_values(g, lds + wave * kTileBytes, last, lane);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const int shift = exp_shift<D>((size_t)min(x * 16 + n, last), quarter);
-        stage_rows(lds, vt_write, x, v[x], shift);
-        scores_rows(s, x, k[x], shift, st);
+        if constexpr (Stream<FMT, D>::kStaged) staged_quarter(g.k[x], k_lds, x, lane);
+        scores_rows(s, x, g.k[x], exp_shift<D>((size_t)min(x * 16 + n, last), quarter), st);
       }
+      if constexpr (Stream<FMT, D>::kStaged) wait_reads();
     };
     request(begin);
     const int full_end = min(pre_end, u.n_keys / 32);   // (only the list's last tile can be a partial one)
     for (int tile = begin; tile < full_end; ++tile) {
       f32x4 s[RB][2];
       consume(s, 31);
-      request(tile + 1);
+      if (tile + 1 < pre_end) request(tile + 1);
       __builtin_amdgcn_sched_barrier(0);
       wave_order();
       attend_rows<D, RB, TILE_FULL>(st, s, lds, vt_read, p.scale_log2, tile * 32, u.n_keys, lane);
@@ -949,31 +1031,23 @@ template <int FMT, int D>
 hipError_t launch(const SparseParams &p, hipStream_t stream) {
   const int64_t units = (int64_t)p.B * p.n_groups * p.n_row_tiles * p.Hkv;
   const dim3 grid((unsigned)(units * p.n_split)), block(64 * p.waves);
-  switch (p.tile_rows * 100 + p.waves) {
-    case 1604: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 1, 4>), grid, block, 0, stream, p); break;
-    case 1608: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 1, 8>), grid, block, 0, stream, p); break;
-    case 3204: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 2, 4>), grid, block, 0, stream, p); break;
-    case 12804:
-      if constexpr (D == 256) {
-        hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 4, 1>), grid, block, 0, stream, p);
-        break;
-      } else {
-        return hipErrorInvalidValue;
-      }
-    default:
-      if constexpr (D < 256) {
-        switch (p.tile_rows * 100 + p.waves) {
-          case 1616: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 1, 16>), grid, block, 0, stream, p); break;
-          case 3208: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 2, 8>), grid, block, 0, stream, p); break;
-          case 6404: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 2, 2>), grid, block, 0, stream, p); break;
-          case 9606: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 3, 2>), grid, block, 0, stream, p); break;
-          case 12808: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 4, 2>), grid, block, 0, stream, p); break;
-          default: return hipErrorInvalidValue;
-        }
-        break;
-      } else {
-        return hipErrorInvalidValue;
-      }
+  const int shape = p.tile_rows * 100 + p.waves;
+  if (shape == 1604) {
+    hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 1, 4>), grid, block, 0, stream, p);
+  } else if (shape == 3204) {
+    hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 2, 4>), grid, block, 0, stream, p);
+  } else if constexpr (D == 256) {
+    if (shape != 12804) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 4, 1>), grid, block, 0, stream, p);
+  } else {
+    switch (shape) {
+      case 1608: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 1, 8>), grid, block, 0, stream, p); break;
+      case 3208: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 2, 8>), grid, block, 0, stream, p); break;
+      case 6404: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 2, 2>), grid, block, 0, stream, p); break;
+      case 9606: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 3, 2>), grid, block, 0, stream, p); break;
+      case 12808: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 4, 2>), grid, block, 0, stream, p); break;
+      default: return hipErrorInvalidValue;
+    }
   }
   return hipGetLastError();
 }

@@ -124,7 +124,7 @@ constexpr SparseShape kShapes[] = {
     {128, 4, 32, 2.0, 2.0},  // (head dimension 256)
 };
 bool shape_fits(const SparseShape &s, int D, int64_t rows) {
-  if (D == 256) return rows <= 16 ? s.rows == 16 : rows <= 32 ? s.rows == 32 && s.waves == 4 : s.rows == 128 && s.waves == 4;
+  if (D == 256) return s.waves == 4 && s.rows == (rows <= 16 ? 16 : rows <= 32 ? 32 : 128);
   if (s.keys == 32 && s.rows == 128) return false;
   return rows <= 16 ? s.rows == 16 : rows <= 32 ? s.rows == 32 : rows <= 64 ? s.rows == 64 : s.rows >= 64;
 }
