@@ -417,7 +417,7 @@ __device__ __forceinline__ void stage_rows(uint8_t *lds, int vt_write, int u, co
 // whose neighbouring lanes read different rows takes one for every lane, one whose lanes read whole rows one for 64 bytes or
 // more.  V comes in whole rows, through registers, and goes to LDS as bf16.  K wants a row for every lane: quantised, a lane's
 // quarter of a row is one or two loads, which is cheaper than a way through LDS (32 requests x 32 blocks, fp4: 17.2 us, through
-// LDS 20.9; groups of one token and 6 rows, fp8: 26.4 us and 28.6; V and K both a row for every lane: 17.1 and 36.6); as
+// LDS 20.9; 54 groups of 5 rows, fp8: 26.4 us and 28.6; V and K both a row for every lane: 17.1 and 36.6); as
 // bf16 it is four, and K goes through LDS as stored (48 requests: 79 us and 105).  There the pieces of a row lie permuted: piece
 // c of key k at c ^ key_mix(k), so that one piece of 16 keys misses no bank.
 template <int FMT, int D>
@@ -488,9 +488,9 @@ __device__ __forceinline__ void staged_quarter(Quarter<FMT_BF16, D> &r, const ui
 }
 
 // Wavefronts of a SIMD that the registers are allotted for: a wavefront alone issues a vector instruction about every other
-// time it could, so as many as the accumulators leave room for.
+// time it could, so as many as the accumulators, and with bf16 the tiles in LDS, leave room for.
 template <int FMT, int D, int RB>
-constexpr int kRowsOccupancy = D == 256 ? (RB == 1 ? 2 : 1) : RB == 2 ? 2 : D == 128 ? 3 : 4;
+constexpr int kRowsOccupancy = D == 256 ? (RB == 1 && FMT != FMT_BF16 ? 2 : 1) : D == 128 ? (RB == 1 && FMT != FMT_BF16 ? 3 : 2) : RB == 2 ? 2 : 4;
 
 template <int FMT, int D, int RB, int NW>
 __global__ __launch_bounds__(64 * NW, (kRowsOccupancy<FMT, D, RB>)) void attn_rows_kernel(const SparseParams p) {

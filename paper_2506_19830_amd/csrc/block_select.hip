@@ -74,7 +74,10 @@ template <int D, int SLOT, int NB>
 __global__ __launch_bounds__(256) void block_score_kernel(const SelectParams p) {
   constexpr int T = D / 16, kShare = 32 / SLOT, kRegs = SLOT / 2;  // groups of a row tile; registers of a group
   constexpr int kPieces = D / 8, kMask = kPieces < 16 ? kPieces - 1 : 15;   // 16-byte pieces of a query row
-  constexpr int kBoundBytes = 32 * 4 * D, kTileBytes = 32 * 2 * D;
+  // The bounds of 32 blocks, lower and upper ones together or, where nothing else wants the LDS, one after the other: a SIMD
+  // then holds four wavefronts instead of two (32 requests of up to 512 blocks: 14.1 -> 13.2 us;
+  // 54 groups of 5 rows and 626 blocks: 9.3 -> 7.6).
+  constexpr int kHalves = SLOT < 32 ? 1 : 2, kTileBytes = 32 * 2 * D, kBoundBytes = kHalves * kTileBytes;
   constexpr int kRing = 4, kPerWave = kTileBytes / 1024 / 4;        // query tiles in LDS; loads of a wavefront per tile
   __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kBoundBytes];
   static_assert(kRing * kTileBytes <= 4 * kBoundBytes, "the query tiles take the place of the bounds");
@@ -122,28 +125,41 @@ __global__ __launch_bounds__(256) void block_score_kernel(const SelectParams p) 
 #pragma unroll
     for (int t = 0; t < T; ++t) q[t] = *(const u32x4 *)(qs + t * 32);
   };
+  auto request_bounds = [&](int nb, int upper) __attribute__((always_inline)) {
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    constexpr int kLanes = D / 4;   // lanes of a block's 4 D bytes
-#pragma unroll
-    for (int i = 0; i < kBoundBytes / 1024; ++i) {
-      const int x = i * (64 / kLanes) + lane / kLanes;             // the block among the 32
+    for (int i = 0; i < kTileBytes / 1024; ++i) {
+      const int x = i * (64 / kPieces) + lane / kPieces;           // the block among the 32
       const int from = __shfl(blk[nb], x);
-      const int piece = (lane % kLanes) ^ (x & 15);
-      load_lds16((const uint8_t *)p.k_bounds + (((size_t)from * p.Hkv + hk) * kLanes + piece) * 16, bounds_at + i * 1024);
+      const int piece = (lane % kPieces) ^ (x & kMask);
+      load_lds16((const uint8_t *)p.k_bounds + ((((size_t)from * p.Hkv + hk) * 2 + upper) * kPieces + piece) * 16,
+                 bounds_at + upper % kHalves * kTileBytes + i * 1024);
     }
-    if (SLOT < 32 && nb == 0) request_rows(first);
-    wait_loads<0>();
-    const uint8_t *mine = lds + wave * kBoundBytes + ln * 4 * D;
+  };
+  auto take_bounds = [&](u32x4 (&x)[T], int upper) __attribute__((always_inline)) {
+    const uint8_t *mine = lds + wave * kBoundBytes + upper % kHalves * kTileBytes + ln * 2 * D;
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      lo[nb][t] = *(const u32x4 *)(mine + (((2 * t + h) ^ (ln & 15)) << 4));
-      hi[nb][t] = *(const u32x4 *)(mine + (((kPieces + 2 * t + h) ^ (ln & 15)) << 4));
-    }
-    // the next tile, and the query rows, come to the same place: this one has to be in registers first
+    for (int t = 0; t < T; ++t) x[t] = *(const u32x4 *)(mine + (((2 * t + h) ^ (ln & kMask)) << 4));
+  };
+  // (what comes next to the same place waits until this is in registers)
+  auto wait_taken = [&]() __attribute__((always_inline)) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
     __builtin_amdgcn_sched_barrier(0);
+  };
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    request_bounds(nb, 0);
+    if (kHalves == 2) request_bounds(nb, 1);
+    if (SLOT < 32 && nb == 0) request_rows(first);
+    wait_loads<0>();
+    take_bounds(lo[nb], 0);
+    if (kHalves == 1) {
+      wait_taken();
+      request_bounds(nb, 1);
+      wait_loads<0>();
+    }
+    take_bounds(hi[nb], 1);
+    wait_taken();
   }
   auto tile_scores = [&](const u32x4 (&q)[T], f32x16 (&s)[NB]) __attribute__((always_inline)) {
 #pragma unroll
@@ -331,6 +347,28 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
       item[k] = i < p.n_max ? score[i] : 0.f;
     }
   }
+  // the largest sum of magnitudes of a row and the largest magnitude of a bound give the error of the scores
+  const int g = group / p.n_groups, t0 = (group - g * p.n_groups) * p.group_len;
+  const int n_rows = min(p.group_len, p.L - t0) * p.G;
+  const size_t tok0 = ((size_t)b * p.gamma + g) * p.L + t0;
+  auto row_of = [&](int r) __attribute__((always_inline)) {
+    return (const uint8_t *)p.q + ((tok0 + r / p.G) * p.Hq + hk * p.G + r % p.G) * D * 2;
+  };
+  float size_q = 0.f, size_k = 0.f;
+  constexpr int kPer = D / 8;  // lanes that share a row
+  for (int i0 = 0; i0 < n_rows * kPer; i0 += NT) {
+    const int i = i0 + tid;
+    float a = 0.f;
+    if (i < n_rows * kPer) {
+      const u32x4 x = *(const u32x4 *)(row_of(i / kPer) + (i % kPer) * 16);
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        a += __builtin_bit_cast(float, x[w] << 16 & 0x7fffffffu) + __builtin_bit_cast(float, x[w] & 0x7fff0000u);
+    }
+#pragma unroll
+    for (int off = 1; off < kPer; off <<= 1) a += __shfl_xor(a, off);
+    size_q = fmaxf(size_q, a);
+  }
   const int n = prefix_blocks(p, b);
   if (n <= p.max_sel) {
     for (int i = tid; i < p.max_sel; i += NT) out[i] = i < n ? i : -1;
@@ -354,31 +392,8 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
     }
   };
 
-  // the largest sum of magnitudes of a row and the largest magnitude of a bound give the error of the scores; the smallest and
-  // the largest key
-  const int g = group / p.n_groups, t0 = (group - g * p.n_groups) * p.group_len;
-  const int n_rows = min(p.group_len, p.L - t0) * p.G;
-  const size_t tok0 = ((size_t)b * p.gamma + g) * p.L + t0;
-  auto row_of = [&](int r) __attribute__((always_inline)) {
-    return (const uint8_t *)p.q + ((tok0 + r / p.G) * p.Hq + hk * p.G + r % p.G) * D * 2;
-  };
-  float size_q = 0.f, size_k = 0.f;
-  constexpr int kPer = D / 8;  // lanes that share a row
-  for (int i0 = 0; i0 < n_rows * kPer; i0 += NT) {
-    const int i = i0 + tid;
-    float a = 0.f;
-    if (i < n_rows * kPer) {
-      const u32x4 x = *(const u32x4 *)(row_of(i / kPer) + (i % kPer) * 16);
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-        a += __builtin_bit_cast(float, x[w] << 16 & 0x7fffffffu) + __builtin_bit_cast(float, x[w] & 0x7fff0000u);
-    }
-#pragma unroll
-    for (int off = 1; off < kPer; off <<= 1) a += __shfl_xor(a, off);
-    size_q = fmaxf(size_q, a);
-  }
   for (int i = tid; i * p.top_blocks < n; i += NT) size_k = fmaxf(size_k, p.top[((size_t)b * p.Hkv + hk) * p.n_tiles + i]);
-  uint32_t key_lo = 0xffffffffu, key_hi = 0;
+  uint32_t key_lo = 0xffffffffu, key_hi = 0;   // the smallest and the largest key
   for_each([&](int, float s, int) { key_lo = min(key_lo, order_key(s)), key_hi = max(key_hi, order_key(s)); });
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
