@@ -12,9 +12,9 @@
 // Probabilities are rounded to bf16 for the second product (relative 2^-9 each, of the size of the output's own rounding);
 // scores, maxima, sums and accumulators are fp32.
 //
-// Two kernels.  With up to 32 rows to a group (attn_rows_kernel) the work is a stream of keys that few rows look at: every
+// Two kernels.  With up to 32 rows to a group (attn_blocks_rows_kernel) the work is a stream of keys that few rows look at: every
 // wavefront takes tiles of 32 keys of its own for all rows, and the wavefronts are folded at the end.  With more rows
-// (attn_tile_kernel) two, three or four pairs of wavefronts with 32 rows each, one for either half of the keys, share tiles
+// (attn_blocks_tile_kernel) two, three or four pairs of wavefronts with 32 rows each, one for either half of the keys, share tiles
 // of 64 keys that they widen into LDS together (head dimension 256: four wavefronts and 32 keys).  Workgroups that share a
 // group's keys leave partial results that the merge of long splits joins.
 #include "attn_common.hpp"
@@ -59,7 +59,7 @@ __device__ __forceinline__ int swizzle(int key) {
   return D == 64 ? (((key >> 1) & 1) << 2) | ((key >> 2) & 3) : ((key & 3) << 2) | ((key >> 2) & 3);
 }
 
-// The same where a store covers whole rows one after the other and a transposing read 16 keys x 32 bytes (attn_rows_kernel): the
+// The same where a store covers whole rows one after the other and a transposing read 16 keys x 32 bytes (attn_blocks_rows_kernel): the
 // pieces of a chunk that a lane widens come one per store, so neighbouring rows differ in the lowest bits.
 template <int D>
 __device__ __forceinline__ int swizzle_rows(int key) {
@@ -216,7 +216,7 @@ __device__ __forceinline__ int block_at(const SparseParams &p, const Unit &u, co
 __device__ __forceinline__ size_t row_at(const SparseParams &p, const Unit &u, int blk, int key) {
   return (((size_t)(uint32_t)blk * (uint32_t)p.Hkv + (uint32_t)u.hk) << p.block_shift) + (min(key, u.n_keys - 1) & ((1 << p.block_shift) - 1));
 }
-// Groups of 16 keys lie in one block.  Where lanes of a wavefront share their keys' groups (attn_rows_kernel), a group's place
+// Groups of 16 keys lie in one block.  Where lanes of a wavefront share their keys' groups (attn_blocks_rows_kernel), a group's place
 // goes through scalar registers, and a lane adds its offset inside the group.
 struct KeyGroup {
   size_t row;   // the group's first row in the cache
@@ -493,7 +493,7 @@ template <int FMT, int D, int RB>
 constexpr int kRowsOccupancy = D == 256 ? (RB == 1 && FMT != FMT_BF16 ? 2 : 1) : D == 128 ? (RB == 1 && FMT != FMT_BF16 ? 3 : 2) : RB == 2 ? 2 : 4;
 
 template <int FMT, int D, int RB, int NW>
-__global__ __launch_bounds__(64 * NW, (kRowsOccupancy<FMT, D, RB>)) void attn_rows_kernel(const SparseParams p) {
+__global__ __launch_bounds__(64 * NW, (kRowsOccupancy<FMT, D, RB>)) void attn_blocks_rows_kernel(const SparseParams p) {
   constexpr int kTileBytes = 32 * D * 2;            // V tile of a wavefront
   constexpr int kKeyBytes = Stream<FMT, D>::kKeyBytes;   // its K tile, as stored
   constexpr int kOne = RB * (D / 16) * 4 * 64;      // floats of one wavefront's accumulators
@@ -862,7 +862,7 @@ __device__ __forceinline__ void tile_step(f32x16 &next, const f32x16 &s, TileRow
 
 // RW wavefronts side by side along the rows, KS along the keys of a tile.
 template <int FMT, int D, int RW, int KS>
-__global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void attn_tile_kernel(const SparseParams p) {
+__global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void attn_blocks_tile_kernel(const SparseParams p) {
   constexpr int KEYS = D == 256 ? 32 : 64, NB = KEYS / 32 / KS, NW = RW * KS;
   static_assert(NB == 1, "every wavefront has 32 keys of a tile");
   constexpr int kTileBytes = KEYS * D * 2;
@@ -1033,19 +1033,19 @@ hipError_t launch(const SparseParams &p, hipStream_t stream) {
   const dim3 grid((unsigned)(units * p.n_split)), block(64 * p.waves);
   const int shape = p.tile_rows * 100 + p.waves;
   if (shape == 1604) {
-    hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 1, 4>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((attn_blocks_rows_kernel<FMT, D, 1, 4>), grid, block, 0, stream, p);
   } else if (shape == 3204) {
-    hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 2, 4>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((attn_blocks_rows_kernel<FMT, D, 2, 4>), grid, block, 0, stream, p);
   } else if constexpr (D == 256) {
     if (shape != 12804) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 4, 1>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((attn_blocks_tile_kernel<FMT, D, 4, 1>), grid, block, 0, stream, p);
   } else {
     switch (shape) {
-      case 1608: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 1, 8>), grid, block, 0, stream, p); break;
-      case 3208: hipLaunchKernelGGL((attn_rows_kernel<FMT, D, 2, 8>), grid, block, 0, stream, p); break;
-      case 6404: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 2, 2>), grid, block, 0, stream, p); break;
-      case 9606: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 3, 2>), grid, block, 0, stream, p); break;
-      case 12808: hipLaunchKernelGGL((attn_tile_kernel<FMT, D, 4, 2>), grid, block, 0, stream, p); break;
+      case 1608: hipLaunchKernelGGL((attn_blocks_rows_kernel<FMT, D, 1, 8>), grid, block, 0, stream, p); break;
+      case 3208: hipLaunchKernelGGL((attn_blocks_rows_kernel<FMT, D, 2, 8>), grid, block, 0, stream, p); break;
+      case 6404: hipLaunchKernelGGL((attn_blocks_tile_kernel<FMT, D, 2, 2>), grid, block, 0, stream, p); break;
+      case 9606: hipLaunchKernelGGL((attn_blocks_tile_kernel<FMT, D, 3, 2>), grid, block, 0, stream, p); break;
+      case 12808: hipLaunchKernelGGL((attn_blocks_tile_kernel<FMT, D, 4, 2>), grid, block, 0, stream, p); break;
       default: return hipErrorInvalidValue;
     }
   }
