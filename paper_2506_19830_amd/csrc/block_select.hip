@@ -272,7 +272,8 @@ struct Shared {
   int doubt[kListed];
   unsigned long long doubt_key[kListed];
   uint8_t doubt_taken[kListed];
-  uint32_t n_pairs, pair[kPairs];
+  uint32_t n_pairs, pair_row[kPairs];   // (a group may have up to 2^30 rows)
+  uint16_t pair_doubt[kPairs];          // index into doubt
   int count[8 * (NT / 64)];
 };
 
@@ -357,11 +358,11 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
   };
   float size_q = 0.f, size_k = 0.f;
   constexpr int kPer = D / 8;  // lanes that share a row
-  for (int i0 = 0; i0 < n_rows * kPer && p.n_max > p.max_sel; i0 += NT) {
-    const int i = i0 + tid;
+  for (int r0 = 0; r0 < n_rows && p.n_max > p.max_sel; r0 += NT / kPer) {
+    const int r = r0 + tid / kPer;
     float a = 0.f;
-    if (i < n_rows * kPer) {
-      const u32x4 x = *(const u32x4 *)(row_of(i / kPer) + (i % kPer) * 16);
+    if (r < n_rows) {
+      const u32x4 x = *(const u32x4 *)(row_of(r) + (tid % kPer) * 16);
 #pragma unroll
       for (int w = 0; w < 4; ++w)
         a += __builtin_bit_cast(float, x[w] << 16 & 0x7fffffffu) + __builtin_bit_cast(float, x[w] & 0x7fff0000u);
@@ -518,9 +519,11 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
             const int r = r0 + (j >> 2) * 8 + h * 4 + (j & 3);
-            if (k < (int)n_doubt && r < n_rows && s[j] >= least) {
+            // (nothing is counted once there are too many: the pairs of many rows and blocks would pass 32 bits)
+            if (k < (int)n_doubt && r < n_rows && s[j] >= least &&
+                __hip_atomic_load(&sh.n_pairs, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) <= kPairs) {
               const uint32_t at = atomicAdd(&sh.n_pairs, 1u);
-              if (at < kPairs) sh.pair[at] = (uint32_t)r * kListed + (uint32_t)k;
+              if (at < kPairs) sh.pair_row[at] = (uint32_t)r, sh.pair_doubt[at] = (uint16_t)k;
             }
           }
         }
@@ -529,17 +532,20 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
       const int n_pairs = (int)sh.n_pairs;
       all_rows = n_pairs > kPairs;
       for (int i0 = wave * 8; i0 < n_pairs && !all_rows; i0 += kWaves * 8) {
-        const uint32_t pair = sh.pair[min(i0 + (lane >> 3), n_pairs - 1)];
-        const double s = exact_row(sh.doubt[pair % kListed], (int)(pair / kListed));
-        if ((lane & 7) == 0) atomicMax(&sh.doubt_key[pair % kListed], (unsigned long long)order_key64(s));
+        const int pair = min(i0 + (lane >> 3), n_pairs - 1), k = sh.pair_doubt[pair];
+        const double s = exact_row(sh.doubt[k], (int)sh.pair_row[pair]);
+        if ((lane & 7) == 0) atomicMax(&sh.doubt_key[k], (unsigned long long)order_key64(s));
       }
     }
     if (n_doubt > need) {
-      const int parts = all_rows ? (n_rows + 7) / 8 : 0;
-      for (int w = wave; w < (int)n_doubt * parts; w += kWaves) {
-        const int k = w / parts;
-        const double s = exact_rows(sh.doubt[k], (w - k * parts) * 8);
+      // (block, part of the rows) in turn, kWaves of them a step; their number may pass 32 bits
+      const int parts = (n_rows + 7) / 8, next_k = kWaves / parts, next_part = kWaves % parts;
+      int k = wave / parts, part = wave % parts;
+      while (all_rows && k < (int)n_doubt) {
+        const double s = exact_rows(sh.doubt[k], part * 8);
         if (lane == 0) atomicMax(&sh.doubt_key[k], (unsigned long long)order_key64(s));
+        k += next_k, part += next_part;
+        if (part >= parts) part -= parts, ++k;
       }
       __syncthreads();
     }

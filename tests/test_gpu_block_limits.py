@@ -1,0 +1,43 @@
+"""The block cache's calls at sizes where an index, a count or a sum could leave its type."""
+import numpy as np
+import pytest
+import torch
+
+import block_cache_util as U
+from paper_2506_19830_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def near_ties(rng, n, D):
+    """Bounds [n, 1, 2, D] whose scores a sum in fp32 cannot tell apart: a large common part, and a small channel that differs."""
+    one = U.bf16(100.0 * rng.standard_normal((1, 1, D)))
+    bounds = U.bf16(np.repeat(np.stack((one - 200.0, one + 200.0), 2), n, 0))
+    for which, sign in ((0, -1.0), (1, 1.0)):
+        bounds[:, 0, which, 5] = U.bf16(sign * 2.0 ** -6 * (1 + rng.permutation(n) % 128 / 128.0))
+    return bounds
+
+
+def test_select_with_more_than_four_million_rows_to_a_group():
+    """The row that decides lies 2^22 rows behind the group's first; the row with its number less 2^22 has another sign and would
+    order the blocks otherwise."""
+    rng = np.random.default_rng(31)
+    G, D, n, most = 8, 64, 40, 9
+    L = (1 << 19) + 40                                        # 2^22 + 320 rows
+    bounds = near_ties(rng, n, D)
+    row = U.bf16(rng.standard_normal((1, 1, 1, D)))
+    q = torch.zeros((1, 1, L, G, D), dtype=torch.bfloat16, device="cuda")
+    at = (1 << 22) + 77
+    q[0, 0, at // G, at % G] = torch.from_numpy(row.ravel()).to(torch.bfloat16).cuda()
+    q[0, 0, 77 // G, 77 % G] = torch.from_numpy(-0.5 * row.ravel()).to(torch.bfloat16).cuda()
+    d = U.desc("bf16", Hq=G, Hkv=1, D=D, L=L, bs=16, max_blocks=n)
+    s = B.make_select_desc(group_len=L, max_blocks=most)
+    blocks = torch.full((1, 1, 1, 1, most), -9, dtype=torch.int32, device="cuda")
+    counts = torch.full((1, 1, 1, 1), -9, dtype=torch.int32, device="cuda")
+    ws = torch.empty(B.la_block_select_workspace(d, s, [16 * n]), dtype=torch.uint8, device="cuda")
+    B.la_block_select(d, s, q, torch.from_numpy(bounds).to(torch.bfloat16).cuda(), None, U.i32([16 * n]), [16 * n], blocks, counts, ws)
+    # (the rows of zeros score nothing, below the two others)
+    want = U.ref_select(np.concatenate((row, -0.5 * row), 2), bounds, n, 1, most, 0, 0)[0]
+    assert U.ref_select(-0.5 * row, bounds, n, 1, most, 0, 0)[0].tolist() != want.tolist()
+    assert counts.item() == most
+    assert blocks.cpu().numpy().ravel().tolist() == want.ravel().tolist()
