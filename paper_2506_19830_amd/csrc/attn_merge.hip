@@ -201,6 +201,8 @@ hipError_t launch_merge(const AttnParams &p, hipStream_t stream) {
 
 }  // namespace
 
+int attn_merge_threads(int D, int s_max) { return s_max <= 8 ? D / 4 : 64; }
+
 hipError_t launch_attn_merge(const AttnParams &p, hipStream_t stream) {
   ProfileScope scope(SLOT_ATTN_MERGE, stream);
   switch (p.D) {

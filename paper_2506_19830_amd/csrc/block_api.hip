@@ -11,8 +11,10 @@ namespace {
 inline bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
-constexpr int64_t kMaxUnits = 1 << 23;   // workgroups per launch (a grid has fewer than 2^32 threads)
-constexpr int64_t kMaxBlocks = 1 << 20;  // blocks of one request that a selection can look at
+constexpr int64_t kMaxUnits = 1 << 23;          // workgroups per launch
+constexpr int64_t kMaxThreads = 0xffffffff;     // and threads: a dimension of a grid has fewer than 2^32
+constexpr int64_t kMaxBlocks = 1 << 20;         // blocks of one request that a selection can look at
+inline bool launchable(int64_t workgroups, int threads) { return workgroups <= kMaxUnits && workgroups * threads <= kMaxThreads; }
 
 // Shape, types and sizes that every call of the block cache checks.
 la_status validate(const la_attn_desc *d) {
@@ -98,7 +100,8 @@ la_status plan_select(const la_attn_desc *d, const la_select_desc *s, const int3
   if ((st = check_prefixes(d, prefix_lens_host, &longest)) != LA_OK) return st;
   const int64_t n = (longest + d->block_size - 1) / d->block_size;
   plan->units = (int64_t)d->num_requests * d->gamma * num_groups(d, s) * d->num_kv_heads;
-  if (plan->units > kMaxUnits || n > kMaxBlocks) return LA_ERR_UNSUPPORTED;
+  if (n > kMaxBlocks) return LA_ERR_UNSUPPORTED;
+  if (!launchable(plan->units, block_pick_threads((int)n, s->group_len * (d->num_q_heads / d->num_kv_heads)))) return LA_ERR_UNSUPPORTED;
   plan->n_max = (int)n, plan->n_tiles = (int)((n + 31) / 32);
   const bool all = n <= s->max_blocks;   // nothing to choose
   plan->score_bytes = all ? 0 : align_up((size_t)plan->units * n * sizeof(float));
@@ -153,7 +156,6 @@ la_status plan_sparse(const la_attn_desc *d, const la_select_desc *s, const int3
     if (!shape_fits(shape, D, rows)) continue;
     const int64_t row_tiles = (rows + shape.rows - 1) / shape.rows;
     const int64_t per_request = (int64_t)plan->n_groups * row_tiles * d->num_kv_heads, units = per_request * d->num_requests;
-    if (units > kMaxUnits) return LA_ERR_UNSUPPORTED;
     // tiles of the longest request's units, and of all (own tokens of the branches that a unit's rows belong to)
     const int64_t own = ((int64_t)d->branch_len + shape.rows) / shape.keys + 2;
     const int64_t most = (most_keys + shape.keys - 1) / shape.keys + own;
@@ -161,13 +163,14 @@ la_status plan_sparse(const la_attn_desc *d, const la_select_desc *s, const int3
     // the blocks of a workgroup's tiles have to fit its table (a range need not begin at a block's first key)
     const int64_t fit = ((int64_t)attn_blocks_max_slots() - 2) * d->block_size / shape.keys - 2;
     const int64_t least = (most + fit - 1) / fit;
-    if (units * least > kMaxUnits) return LA_ERR_UNSUPPORTED;
+    if (!launchable(units * least, 64 * shape.waves)) continue;
     // all CUs stream at 5 TB/s between them
     const double scale = D / 128.0, stream = shape.keys * row_bytes * cus / 5.0e6;
     const double busy = shape.busy * scale > stream ? shape.busy * scale : stream;
     const double alone = shape.latency * scale > busy ? shape.latency * scale : busy;
     const int64_t slots = most / (shape.keys == 32 ? shape.waves : 1);   // a tile at least for every wavefront
     for (int64_t n = least; n == least || (n <= slots && n <= 64 && units * n <= 4 * (int64_t)cus); ++n) {
+      if (n > 1 && (int64_t)all_rows * attn_merge_threads(D, (int)n) > kMaxThreads - 255) break;
       const double start = 1.5, longest_us = (double)most / (double)n * alone + start;
       const double all_us = (double)per_request / cus * (tiles * busy + (double)(n * d->num_requests) * start);
       const double merge_us = n > 1 ? 3.0 + (double)(n * all_rows) * (D + 2) * 8.0 / 3.0e6 : 0.0;
@@ -183,6 +186,7 @@ la_status plan_sparse(const la_attn_desc *d, const la_select_desc *s, const int3
       }
     }
   }
+  if (best < 0.0) return LA_ERR_UNSUPPORTED;   // more workgroups than a launch takes, whatever the shape
   const size_t n = (size_t)plan->n_split;
   plan->part_o_bytes = n > 1 ? align_up(n * all_rows * D * sizeof(float)) : 0;
   plan->part_ml_bytes = n > 1 ? align_up(n * all_rows * 2 * sizeof(float)) : 0;
@@ -235,7 +239,7 @@ la_status la_kv_store(const la_attn_desc *desc, const la_block_cache *cache, con
   }
   // rows that begin anywhere in a block touch at most this many
   p.n_dst = (int)((tokens + desc->block_size - 2) / desc->block_size) + 1;
-  if ((int64_t)p.n_dst * desc->num_kv_heads > kMaxUnits) return LA_ERR_UNSUPPORTED;
+  if (!launchable((int64_t)p.n_dst * desc->num_kv_heads, 256)) return LA_ERR_UNSUPPORTED;
   return launch_kv_store(p, format_of(desc), (hipStream_t)hip_stream) == hipSuccess ? LA_OK : LA_ERR_LAUNCH;
 }
 

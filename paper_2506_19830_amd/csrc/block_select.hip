@@ -697,10 +697,9 @@ hipError_t launch(SelectParams p, hipStream_t stream) {
   }
   ProfileScope scope(SLOT_BLOCK_PICK, stream);
   const dim3 grid((unsigned)((int64_t)p.B * p.gamma * p.n_groups * p.Hkv));
-  // sixteen wavefronts where one group's work can use them: more candidates than four hold, or exact scores over many rows
   if (p.n_max > 8 * 1024)
     hipLaunchKernelGGL((block_pick_kernel<D, 1024, false>), grid, dim3(1024), 0, stream, p);
-  else if (p.n_max > 8 * 256 || rows > 64)
+  else if (block_pick_threads(p.n_max, rows) == 1024)
     hipLaunchKernelGGL((block_pick_kernel<D, 1024, true>), grid, dim3(1024), 0, stream, p);
   else
     hipLaunchKernelGGL((block_pick_kernel<D, 256, true>), grid, dim3(256), 0, stream, p);
@@ -708,6 +707,9 @@ hipError_t launch(SelectParams p, hipStream_t stream) {
 }
 
 }  // namespace
+
+// Sixteen wavefronts where one group's work can use them: more candidates than four hold, or exact scores over many rows.
+int block_pick_threads(int n_max, int rows) { return n_max > 8 * 256 || rows > 64 ? 1024 : 256; }
 
 hipError_t launch_block_select(const SelectParams &p, hipStream_t stream) {
   switch (p.D) {

@@ -126,6 +126,7 @@ int attn_stream_max_chunk_blocks();
 bool attn_stream_shape_is_fp8(int shape);  // else: bf16 cache and branch K/V
 hipError_t launch_attn_stream(const AttnParams &p, int shape, hipStream_t stream);
 hipError_t launch_attn_merge(const AttnParams &p, hipStream_t stream);
+int attn_merge_threads(int D, int s_max);  // threads per output row of that launch (whose workgroups are 256)
 // row_blocks: blocks of 16 query rows per workgroup (p.n_row_tiles counts those workgroups)
 hipError_t launch_attn_f32(const AttnParams &p, int row_blocks, hipStream_t stream);
 // the same, one wavefront per query row: at most attn_rows_max() rows over all requests, never split
@@ -245,6 +246,8 @@ struct SelectParams {
   int score_groups, score_chunks, top_blocks;
 };
 hipError_t launch_block_select(const SelectParams &p, hipStream_t stream);
+// threads of the workgroup that picks a group's blocks (rows: of a full group)
+int block_pick_threads(int n_max, int rows);
 
 // Attention over selected blocks (sel == null: all blocks of the prefix).  A unit is one (request, group, KV head, tile of
 // the group's rows); without a selection one group holds the rows of all branches.  Its keys, the selected prefix rows and

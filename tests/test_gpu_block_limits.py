@@ -41,3 +41,26 @@ def test_select_with_more_than_four_million_rows_to_a_group():
     assert U.ref_select(-0.5 * row, bounds, n, 1, most, 0, 0)[0].tolist() != want.tolist()
     assert counts.item() == most
     assert blocks.cpu().numpy().ravel().tolist() == want.ravel().tolist()
+
+
+def test_attention_of_two_to_the_23_groups():
+    """As many workgroups as a launch may have, a row each: eight wavefronts to a workgroup would be 2^32 threads."""
+    gamma, H, D, bs, P = 1 << 20, 8, 64, 16, 13
+    g = torch.Generator(device="cuda").manual_seed(11)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    k, v = rand(1, H, bs, D), rand(1, H, bs, D)
+    q, kb, vb = rand(1, gamma, 1, H, D), rand(1, gamma, 1, H, D), rand(1, gamma, 1, H, D)
+    d = U.desc("bf16", Hq=H, Hkv=H, D=D, gamma=gamma, L=1, bs=bs, max_blocks=1)
+    s = B.make_select_desc(group_len=1, max_blocks=1)
+    blocks = torch.zeros((1, gamma, 1, H, 1), dtype=torch.int32, device="cuda")
+    counts = torch.ones((1, gamma, 1, H), dtype=torch.int32, device="cuda")
+    out, lse = torch.full_like(q, float("nan")), torch.full(q.shape[:-1], float("nan"), device="cuda")
+    ws = torch.empty(max(16, B.la_verify_attention_sparse_workspace(d, s, [P])), dtype=torch.uint8, device="cuda")
+    B.la_verify_attention_sparse(d, s, q, B.make_block_cache(k, v), None, U.i32([P]), [P], blocks, counts, kb, vb, out, lse, ws)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    at = np.concatenate((np.arange(5), np.random.default_rng(2).integers(0, gamma, 200), gamma - 1 - np.arange(5)))
+    up = lambda x: x.double().cpu().numpy()  # noqa: E731
+    here = torch.from_numpy(at).cuda()
+    ref = U.ref_attend(*(up(x) for x in (q[0, here], k[0, :, :P].transpose(0, 1), v[0, :, :P].transpose(0, 1), kb[0, here], vb[0, here])),
+                       None, bs, 1, float(np.float32(D ** -0.5)))
+    U.check_attend(up(out[0, here]), up(lse[0, here]), ref, D)
