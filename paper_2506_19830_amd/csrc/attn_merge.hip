@@ -97,8 +97,9 @@ __global__ __launch_bounds__(64 * kWaves) void attn_merge_kernel(const AttnParam
     };
     request(0);
     const float m_new = fmaxf(m_all, wave_max(m));
-    const float w = (lane < cnt) ? __builtin_amdgcn_exp2f(m - m_new) : 0.f;
-    const float rescale = __builtin_amdgcn_exp2f(m_all - m_new);  // 0 on the first pass (m_all = -inf)
+    const float base = m_new == -INFINITY ? 0.f : m_new;  // the row saw no key in any chunk so far: every weight is 0
+    const float w = (lane < cnt) ? __builtin_amdgcn_exp2f(m - base) : 0.f;
+    const float rescale = __builtin_amdgcn_exp2f(m_all - base);  // 0 on the first pass (m_all = -inf)
     acc *= rescale;
     denom = denom * rescale + wave_sum(w * l);
     m_all = m_new;

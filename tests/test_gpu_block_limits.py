@@ -64,3 +64,37 @@ def test_attention_of_two_to_the_23_groups():
     ref = U.ref_attend(*(up(x) for x in (q[0, here], k[0, :, :P].transpose(0, 1), v[0, :, :P].transpose(0, 1), kb[0, here], vb[0, here])),
                        None, bs, 1, float(np.float32(D ** -0.5)))
     U.check_attend(up(out[0, here]), up(lse[0, here]), ref, D)
+
+
+def test_a_row_that_sees_nothing_in_the_first_64_splits():
+    """A prefix of more keys than 64 workgroups' tables hold, beside a request without a prefix and two long branches: tiles of rows
+    reach over both branches, and the second one's rows see nothing of what the first 64 workgroups look at."""
+    P, gamma, L, D, bs = 1_200_000, 2, 6000, 64, 16
+    g = torch.Generator(device="cuda").manual_seed(7)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    n_blocks = P // bs
+    k, v = rand(n_blocks, 1, bs, D), rand(n_blocks, 1, bs, D)
+    table = torch.stack((torch.randperm(n_blocks, generator=g, device="cuda"), torch.zeros(n_blocks, device="cuda"))).to(torch.int32)
+    q, kb, vb = rand(2, gamma, L, 1, D), rand(2, gamma, L, 1, D), rand(2, gamma, L, 1, D)
+    d = U.desc("bf16", B_=2, Hq=1, Hkv=1, D=D, gamma=gamma, L=L, bs=bs, max_blocks=n_blocks)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:-1], device="cuda")
+    need = B.la_verify_attention_sparse_workspace(d, None, [P, 0])
+    assert need >= 65 * 2 * gamma * L * (D + 2) * 4           # more than 64 partial results of every row
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    B.la_verify_attention_sparse(d, None, q, B.make_block_cache(k, v), table, U.i32([P, 0]), [P, 0], None, None, kb, vb, out, lse, ws)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    scale = float(np.float32(D ** -0.5))
+    for b, branch, rows in ((1, 0, slice(None)), (1, 1, slice(None)), (0, 0, [0, 5999]), (0, 1, [0, 17, 5999])):
+        kk, vv = (x[b, branch, :, 0].double() for x in (kb, vb))
+        at = torch.arange(L, device="cuda")[rows]
+        seen = torch.arange(L, device="cuda") <= at[:, None]
+        if b == 0:
+            prefix = [x[table[0].long()].reshape(P, D).double() for x in (k, v)]
+            kk, vv = torch.cat((prefix[0], kk)), torch.cat((prefix[1], vv))
+            seen = torch.cat((torch.ones((len(at), P), dtype=torch.bool, device="cuda"), seen), 1)
+        x = q[b, branch, at, 0].double()
+        score = (x @ kk.T.contiguous() * scale).masked_fill(~seen, -np.inf)
+        size = (x.abs() @ kk.abs().T.contiguous() * scale).masked_fill(~seen, 0.0).amax(1)
+        p = torch.softmax(score, 1)
+        ref = [t.cpu().numpy() for t in (p @ vv, torch.logsumexp(score, 1), p @ vv.abs(), size)]
+        U.check_attend(out[b, branch, at, 0].double().cpu().numpy(), lse[b, branch, at, 0].double().cpu().numpy(), ref, D)
