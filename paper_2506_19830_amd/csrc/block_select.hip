@@ -411,6 +411,8 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
     key_lo = min(key_lo, sh.key_lo[w]), key_hi = max(key_hi, sh.key_hi[w]);
   }
   const float err = kScoreError<D> * 1.01f * size_q * size_k + 1e-30f;
+  // where a sum may have left fp32 the rounded scores say nothing: every block is in doubt  (size_q: its own sum may have, too)
+  const bool lost = size_q * size_k > 0x1p126f || size_q > 0x1p126f;
 
   // t, the score of rank `want`: bins of equal width between the smallest and the largest key, then inside the bin it lies in,
   // until a wavefront can hold that
@@ -448,11 +450,12 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
   }
   const float t = key_value(key_lo);
   const float sure = t + 2.f * err, out_of = t - 2.f * err;  // above: certainly taken; below: certainly not
-  auto in_doubt = [&](float s) __attribute__((always_inline)) { return s >= out_of && !(s > sure); };
+  auto taken = [&](float s) __attribute__((always_inline)) { return s > sure && !lost; };
+  auto in_doubt = [&](float s) __attribute__((always_inline)) { return (s >= out_of && !(s > sure)) || lost; };
 
   int slot[kItems];
   for_each([&](int i, float s, int k) {
-    if (s > sure) {
+    if (taken(s)) {
       atomicAdd(&sh.n_sure, 1u);
     } else if (in_doubt(s)) {
       const uint32_t at = atomicAdd(&sh.n_doubt, 1u);
@@ -520,7 +523,7 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
           for (int j = 0; j < 16; ++j) {
             const int r = r0 + (j >> 2) * 8 + h * 4 + (j & 3);
             // (nothing is counted once there are too many: the pairs of many rows and blocks would pass 32 bits)
-            if (k < (int)n_doubt && r < n_rows && s[j] >= least &&
+            if (k < (int)n_doubt && r < n_rows && (s[j] >= least || lost) &&
                 __hip_atomic_load(&sh.n_pairs, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) <= kPairs) {
               const uint32_t at = atomicAdd(&sh.n_pairs, 1u);
               if (at < kPairs) sh.pair_row[at] = (uint32_t)r, sh.pair_doubt[at] = (uint16_t)k;
@@ -567,7 +570,7 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
       bool take = false;
-      if (c0 + tid + k * NT < c1) take = item[k] > sure || (in_doubt(item[k]) && sh.doubt_taken[slot[k]]);
+      if (c0 + tid + k * NT < c1) take = taken(item[k]) || (in_doubt(item[k]) && sh.doubt_taken[slot[k]]);
       const uint64_t mask = __builtin_amdgcn_ballot_w64(take);
       if (lane == 0) sh.count[k * kWaves + wave] = __popcll(mask);
       takes |= (uint32_t)take << k;
@@ -635,7 +638,7 @@ __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
     bool take = false, tie = false;
     if (i < c1) {
       const float s = score[i];
-      take = s > sure;
+      take = taken(s);
       if (!take && in_doubt(s)) {
         if (n_doubt > need) {
           const unsigned long long k = order_key64(exact[i]);

@@ -5,6 +5,7 @@ import torch
 
 import block_cache_util as U
 from paper_2506_19830_amd import binding as B
+from test_gpu_block_select import run_select
 
 pytestmark = pytest.mark.gpu
 
@@ -98,3 +99,27 @@ def test_a_row_that_sees_nothing_in_the_first_64_splits():
         p = torch.softmax(score, 1)
         ref = [t.cpu().numpy() for t in (p @ vv, torch.logsumexp(score, 1), p @ vv.abs(), size)]
         U.check_attend(out[b, branch, at, 0].double().cpu().numpy(), lse[b, branch, at, 0].double().cpu().numpy(), ref, D)
+
+
+@pytest.mark.parametrize("rows,n", [(1, 60), (20, 60), (80, 300), (2, 8300)])
+@pytest.mark.parametrize("where", ["everywhere", "one channel", "one block"])
+def test_select_where_fp32_sums_overflow(rows, n, where):
+    """Finite queries and bounds whose scores, or parts of them, lie beyond fp32: the order is still that of the exact scores, and
+    the list is written whole."""
+    rng = np.random.default_rng(rows + n)
+    D, bs = 64, 16
+    q = U.bf16(rng.standard_normal((1, 1, rows, 1, D)))
+    c = rng.standard_normal((n, 1, D))
+    bounds = U.bf16(np.stack((c - 1.0 - rng.random(c.shape), c + 1.0 + rng.random(c.shape)), 2))
+    big = 2.0 ** 70
+    if where == "everywhere":
+        q, bounds = q * big, bounds * big
+    elif where == "one channel":
+        q[..., 3] *= big
+        bounds[..., 3] *= big
+    else:
+        q *= big
+        bounds[n // 2] *= big
+        bounds[n // 2, :, 0] *= -1.0                          # (bounds that are no bounds: one sum of both infinities)
+    run_select(q, [bounds], [n * bs], 1, bs, rows, 7, 1, 1)
+    run_select(q, [bounds], [n * bs], 1, bs, rows, min(n - 1, 1100), 0, 0)
