@@ -102,6 +102,19 @@ LA_API la_status la_selftest_second_attempt(int on);
 LA_API la_status la_selftest_exhaustive_plans(int on);
 
 /* ------------------------------------------------------------------------- *
+ *  Self-test hook for la_verify_attention_sparse.  It chooses among kernel
+ *  shapes (16, 32, 64, 96 or 128 query rows and 4, 6 or 8 wavefronts to a
+ *  workgroup) and over how many workgroups a group's keys are split by a
+ *  model of their times.  With rows > 0 the calls that follow, and their
+ *  workspace queries, take the shape of `rows` and `waves` (where there is
+ *  none at the head dimension: LA_ERR_UNSUPPORTED) and `split` workgroups, or
+ *  more where a workgroup could not hold its share, so that small calls test
+ *  every shape.  Process-wide, host side only; 0, 0, 0 restores the normal
+ *  behaviour.  LA_ERR_INVALID_ARG for negative values.
+ * ------------------------------------------------------------------------- */
+LA_API la_status la_selftest_sparse_plan(int32_t rows, int32_t waves, int32_t split);
+
+/* ------------------------------------------------------------------------- *
  *  Index checks (debug aid).  The compute calls trust the indices the caller
  *  hands them -- cache block ids and drafted token ids are not range-checked
  *  on the device -- and a checked build of an application can run these two

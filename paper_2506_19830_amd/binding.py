@@ -37,7 +37,8 @@ EXPORTED_SYMBOLS = (
 # what libla_verify_bench.so exports on top of those (la_verify_bench.h)
 BENCH_SYMBOLS = (
     "la_calibrate_mfma", "la_calibrate_mfma_data", "la_calibrate_read", "la_calibrate_issue", "la_selftest_exp64",
-    "la_selftest_accept_table", "la_selftest_force_table", "la_selftest_second_attempt", "la_selftest_exhaustive_plans", "la_check_block_tables", "la_check_draft_tokens",
+    "la_selftest_accept_table", "la_selftest_force_table", "la_selftest_second_attempt", "la_selftest_exhaustive_plans",
+    "la_selftest_sparse_plan", "la_check_block_tables", "la_check_draft_tokens",
     "la_profile_enable", "la_profile_select",
     "la_profile_collect", "la_profile_num_kernels", "la_profile_get", "la_profile_reset",
 )
@@ -530,6 +531,17 @@ def la_selftest_exhaustive_plans(on: bool) -> None:
     st = lib.la_selftest_exhaustive_plans(int(bool(on)))
     if st:
         raise LaError(st, "la_selftest_exhaustive_plans")
+
+
+def la_selftest_sparse_plan(rows: int = 0, waves: int = 0, split: int = 0) -> None:
+    """Make la_verify_attention_sparse run the shape of that many rows and wavefronts to a workgroup, and split a group's keys
+    over ``split`` workgroups, in the calls that follow; without arguments: as it chooses."""
+    lib = load("bench")
+    lib.la_selftest_sparse_plan.restype = ctypes.c_int
+    lib.la_selftest_sparse_plan.argtypes = [ctypes.c_int32] * 3
+    st = lib.la_selftest_sparse_plan(rows, waves, split)
+    if st:
+        raise LaError(st, "la_selftest_sparse_plan")
 
 
 def la_check_block_tables(desc: la_attn_desc, block_tables, prefix_lens_host: Sequence[int], num_cache_blocks: int,

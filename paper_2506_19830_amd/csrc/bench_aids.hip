@@ -20,6 +20,7 @@ struct ProfileRecord {
 // process-wide state of the timing aid (not thread-safe, as its header says)
 bool g_profile_on = false;
 int g_force_second_attempt = 0, g_exhaustive_plans = 0, g_force_table = 0;
+SparseForce g_sparse_force = {0, 0, 0};
 uint32_t g_profile_mask = 0xffffffffu;      // slots that are timed
 int g_profile_stride = 1;                   // of their launches, every stride-th one
 int64_t g_seen[SLOT_COUNT];                 // launches of a slot seen while enabled
@@ -67,6 +68,10 @@ void profile_after(int slot, hipStream_t stream, void *start) {
 int selftest_force_second_attempt() { return g_force_second_attempt; }
 int selftest_force_table() { return g_force_table; }
 int selftest_exhaustive_plans() { return g_exhaustive_plans; }
+bool selftest_sparse_plan(SparseForce *out) {
+  *out = g_sparse_force;
+  return g_sparse_force.rows > 0;
+}
 
 }  // namespace la
 
@@ -109,6 +114,12 @@ la_status la_selftest_second_attempt(int on) {
 
 la_status la_selftest_exhaustive_plans(int on) {
   g_exhaustive_plans = on != 0;
+  return LA_OK;
+}
+
+la_status la_selftest_sparse_plan(int32_t rows, int32_t waves, int32_t split) {
+  if (rows < 0 || waves < 0 || split < 0) return LA_ERR_INVALID_ARG;
+  g_sparse_force = {rows, waves, split};
   return LA_OK;
 }
 

@@ -126,9 +126,10 @@ constexpr SparseShape kShapes[] = {
     {64, 4, 64, 1.30, 0.83}, {96, 6, 64, 1.20, 1.20}, {128, 8, 64, 1.30, 1.30},
     {128, 4, 32, 2.0, 2.0},  // (head dimension 256)
 };
+bool shape_exists(const SparseShape &s, int D) { return D == 256 ? s.waves == 4 && s.keys == 32 : s.keys == 64 || s.rows <= 32; }
 bool shape_fits(const SparseShape &s, int D, int64_t rows) {
-  if (D == 256) return s.waves == 4 && s.rows == (rows <= 16 ? 16 : rows <= 32 ? 32 : 128);
-  if (s.keys == 32 && s.rows == 128) return false;
+  if (!shape_exists(s, D)) return false;
+  if (D == 256) return s.rows == (rows <= 16 ? 16 : rows <= 32 ? 32 : 128);
   return rows <= 16 ? s.rows == 16 : rows <= 32 ? s.rows == 32 : rows <= 64 ? s.rows == 64 : s.rows >= 64;
 }
 
@@ -152,8 +153,10 @@ la_status plan_sparse(const la_attn_desc *d, const la_select_desc *s, const int3
   plan->n_groups = s ? d->gamma * num_groups(d, s) : 1;
   const int cus = num_cus();
   double best = -1.0;
+  SparseForce force = {0, 0, 0};
+  const bool forced = selftest_sparse_plan && selftest_sparse_plan(&force);
   for (const SparseShape &shape : kShapes) {
-    if (!shape_fits(shape, D, rows)) continue;
+    if (forced ? !shape_exists(shape, D) || shape.rows != force.rows || shape.waves != force.waves : !shape_fits(shape, D, rows)) continue;
     const int64_t row_tiles = (rows + shape.rows - 1) / shape.rows;
     const int64_t per_request = (int64_t)plan->n_groups * row_tiles * d->num_kv_heads, units = per_request * d->num_requests;
     // tiles of the longest request's units, and of all (own tokens of the branches that a unit's rows belong to)
@@ -169,7 +172,8 @@ la_status plan_sparse(const la_attn_desc *d, const la_select_desc *s, const int3
     const double busy = shape.busy * scale > stream ? shape.busy * scale : stream;
     const double alone = shape.latency * scale > busy ? shape.latency * scale : busy;
     const int64_t slots = most / (shape.keys == 32 ? shape.waves : 1);   // a tile at least for every wavefront
-    for (int64_t n = least; n == least || (n <= slots && n <= 64 && units * n <= 4 * (int64_t)cus); ++n) {
+    const int64_t n0 = forced && force.split > least ? force.split : least;
+    for (int64_t n = n0; n == n0 || (!forced && n <= slots && n <= 64 && units * n <= 4 * (int64_t)cus); ++n) {
       if (n > 1 && (int64_t)all_rows * attn_merge_threads(D, (int)n) > kMaxThreads - 255) break;
       const double start = 1.5, longest_us = (double)most / (double)n * alone + start;
       const double all_us = (double)per_request / cus * (tiles * busy + (double)(n * d->num_requests) * start);

@@ -282,6 +282,12 @@ __attribute__((weak)) int selftest_force_second_attempt();
 __attribute__((weak)) int selftest_force_table();
 // self-test hook of the benchmark library: nonzero = the planner looks at every number of chunks up to its limit
 __attribute__((weak)) int selftest_exhaustive_plans();
+// self-test hook of the benchmark library: true = attention over blocks runs this shape, over `split` workgroups to a unit where
+// the unit's keys do not need more
+struct SparseForce {
+  int rows, waves, split;
+};
+__attribute__((weak)) bool selftest_sparse_plan(SparseForce *out);
 
 struct ProfileScope {
   int slot;

@@ -54,3 +54,23 @@ def test_attention_over_lists():
     for units, accepted in (((1 << 23) - 8, True), (1 << 23, True), ((1 << 23) + 8, False)):
         d = U.desc("mxfp4_e2m1", Hq=8, Hkv=8, D=64, gamma=units // 8, bs=16, max_blocks=1)
         assert (answer(B.la_verify_attention_sparse_workspace, d, s, [16]) is not None) == accepted
+
+
+def test_forced_shapes():
+    """The self-test hook: shapes that a head dimension does not have are refused, and the choice comes back."""
+    B.select_library("bench")
+    try:
+        s = B.make_select_desc(group_len=1, max_blocks=4)
+        want = {D: B.la_verify_attention_sparse_workspace(U.desc("bf16", D=D), s, [100]) for D in (64, 256)}
+        for D, shape, exists in ((64, (16, 4), True), (64, (128, 8), True), (64, (128, 4), False), (64, (48, 4), False),
+                                 (256, (128, 4), True), (256, (16, 8), False), (256, (64, 4), False)):
+            B.la_selftest_sparse_plan(*shape, 2)
+            got = answer(B.la_verify_attention_sparse_workspace, U.desc("bf16", D=D), s, [100])
+            assert got is None if not exists else got >= 2 * 4 * (D + 2) * 4
+        with pytest.raises(B.LaError):
+            B.la_selftest_sparse_plan(-1, 4, 1)
+        B.la_selftest_sparse_plan()
+        assert want == {D: B.la_verify_attention_sparse_workspace(U.desc("bf16", D=D), s, [100]) for D in (64, 256)}
+    finally:
+        B.la_selftest_sparse_plan()
+        B.select_library("product")
