@@ -336,7 +336,13 @@ LA_API la_status la_kv_commit_tree(
  *  head_dim 64 / 128 / 256; q and the branch's (chain's) K and V bf16.  A bf16
  *  block cache is laid out as la_verify_attention's.  The other conventions are
  *  the header's: what is not finite gives undefined values, block ids are
- *  trusted, desc->kv_split_tokens and kernel_shape must be 0.
+ *  trusted, desc->kv_split_tokens and kernel_shape must be 0.  A call of more
+ *  groups, tiles of rows or blocks to write than a launch holds (2^23
+ *  workgroups, fewer than 2^32 threads: 2^22 - 1 groups, counted per KV head,
+ *  where block selection has more than 64 rows to a group or a prefix of more
+ *  than 2048 blocks) is LA_ERR_UNSUPPORTED, from the workspace query on.  Draft
+ *  trees' accepted paths and nested or tree-shaped branches have no block-cache
+ *  form.
  * ------------------------------------------------------------------------- */
 typedef struct {
   void *k, *v;              /* dev [num_blocks, Hkv, block_size, D] elements, of layer 0           */
@@ -387,8 +393,8 @@ LA_API la_status la_kv_load(
  * ceil(prefix_lens / block_size) blocks max_blocks are listed (all, if there
  * are no more): the first keep_first, the last keep_last, and of the others
  * those with the largest scores, equal ones in the order of their index.  The
- * order is that of the exact scores (fp64 where rounded ones do not settle it),
- * not of rounded ones. */
+ * order is that of the exact scores (fp64 where rounded ones do not settle it,
+ * or may lie beyond fp32), not of rounded ones. */
 typedef struct {
   int32_t group_len;      /* 1..branch_len                                     */
   int32_t max_blocks;     /* >= 1                                              */
@@ -414,8 +420,10 @@ LA_API la_status la_block_select(
  * ascending order (la_block_select's, or the caller's own); counts outside
  * 0..max_blocks and ids outside the prefix are clamped.  blocks == NULL (then
  * sel and counts are NULL too): every block of the prefix.  Probabilities are
- * rounded to bf16 before they meet V, as on la_verify_attention's MFMA path;
- * lse is fp32-accurate.  out_dtype LA_BF16 or LA_F32. */
+ * rounded to bf16 before they meet V at every head dimension and for both
+ * out_dtypes (LA_BF16, LA_F32), as on la_verify_attention's MFMA path; that
+ * call's general path, which runs a bf16 cache at head dimensions 64 and 256,
+ * is fp32-accurate, this one is not.  lse is fp32-accurate. */
 LA_API la_status la_verify_attention_sparse_workspace(const la_attn_desc *desc, const la_select_desc *sel,
                                                       const int32_t *prefix_lens_host, size_t *bytes_out);
 LA_API la_status la_verify_attention_sparse(

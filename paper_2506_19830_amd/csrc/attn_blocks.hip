@@ -9,8 +9,9 @@
 // so that a lane holds scores of one row only, and P^T leaves the accumulators of the first product in the order in which
 // the second one wants its operand (the keys of a tile are permuted alike on both sides).  V lies in LDS as bf16 and is read
 // back transposed by 16-bit reads.  Quantised rows are widened to bf16 exactly, their exponents applied by the conversion.
-// Probabilities are rounded to bf16 for the second product (relative 2^-9 each, of the size of the output's own rounding);
-// scores, maxima, sums and accumulators are fp32.
+// Probabilities are rounded to bf16 for the second product, at every head dimension and for fp32 results too (relative 2^-8 each
+// at most, the output's own rounding where that is bf16; 2.3e-3 of a row's size from the definition, 1.7e-3 with the output's
+// rounding alone): a second term would double the second product.  Scores, maxima, sums and accumulators are fp32.
 //
 // Two kernels.  With up to 32 rows to a group (attn_blocks_rows_kernel) the work is a stream of keys that few rows look at: every
 // wavefront takes tiles of 32 keys of its own for all rows, and the wavefronts are folded at the end.  With more rows
@@ -494,7 +495,7 @@ constexpr int kRowsOccupancy = D == 256 ? (RB == 1 && FMT != FMT_BF16 ? 2 : 1) :
 
 // RB blocks of 16 rows, NW wavefronts with tiles of their own.  Bound by the stream of keys where it is long (fp4, 32 requests x 8
 // heads x 2048 keys: 17.2 us, 4.2 TB/s; fp8, 8 prefixes of 8K to 32K keys: 70 us, 4.3 TB/s), by conversions and cache reads where
-// groups share the keys (fp8, 54 groups x 8 heads x 2048 keys: 27 us).
+// groups share the keys (fp8, 54 groups x 8 heads x 2048 keys: 28.4 us, 26.4 among other calls).
 template <int FMT, int D, int RB, int NW>
 __global__ __launch_bounds__(64 * NW, (kRowsOccupancy<FMT, D, RB>)) void attn_blocks_rows_kernel(const SparseParams p) {
   constexpr int kTileBytes = 32 * D * 2;            // V tile of a wavefront
@@ -864,8 +865,8 @@ __device__ __forceinline__ void tile_step(f32x16 &next, const f32x16 &s, TileRow
 }
 
 // RW wavefronts side by side along the rows, KS along the keys of a tile.  LDS reads, exponentials and matrix instructions of a
-// step each take about a third of its time and overlap in part only: 320 rows x 64 groups x 2048 keys, bf16: 53 us, 415 TFLOP/s
-// (scores, exponentials and values one after the other: 55).
+// step each take about a third of its time and overlap in part only: 320 rows x 64 groups x 2048 keys, bf16, 96 rows to a
+// workgroup: 53 us among other calls, 415 TFLOP/s (scores, exponentials and values one after the other: 55), 58 alone.
 template <int FMT, int D, int RW, int KS>
 __global__ __launch_bounds__(64 * RW * KS, D == 256 ? 1 : 2) void attn_blocks_tile_kernel(const SparseParams p) {
   constexpr int KEYS = D == 256 ? 32 : 64, NB = KEYS / 32 / KS, NW = RW * KS;

@@ -134,8 +134,9 @@ bool shape_fits(const SparseShape &s, int D, int64_t rows) {
 }
 
 // Which shape runs a call and over how many workgroups a unit's keys are split, from a simple model in microseconds (constants
-// fitted to measured times of forced shapes and splits): what the workgroups of all units take, shared out over the CUs, or the longest
-// of them, whichever is more, and the merge of the partial results.
+// fitted to measured times of forced shapes and splits at head dimension 128, scaled to the others): what the workgroups of all
+// units take, shared out over the CUs, or the longest of them, whichever is more, and the merge of the partial results.  Of 15 calls
+// nine take up to 6 % longer than with the fastest shape and split, the others 9 to 34 %.
 la_status plan_sparse(const la_attn_desc *d, const la_select_desc *s, const int32_t *prefix_lens_host, SparsePlan *plan) {
   la_status st = validate(d);
   if (st != LA_OK) return st;

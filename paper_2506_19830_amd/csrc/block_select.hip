@@ -325,8 +325,8 @@ __device__ Key key_of_rank(Shared<NT> &sh, uint32_t rank, F for_each, uint32_t *
 }
 
 // One workgroup picks the blocks of one group and KV head from their scores.  Up to 8 NT candidates stay in registers (IN_REG).
-// Bound by the latency of a dozen dependent steps over a few hundred numbers (256 groups, up to 512 candidates: 9.1 us), and with
-// many rows by the second look at the blocks in doubt (64 groups of 320 rows, 2048 candidates: 20.5 us).
+// Bound by the latency of a dozen dependent steps over a few hundred numbers (256 groups, up to 512 candidates: 9.8 us), and with
+// many rows by the second look at the blocks in doubt (64 groups of 320 rows, 2048 candidates: 20.8 us).
 template <int D, int NT, bool IN_REG>
 __global__ __launch_bounds__(NT) void block_pick_kernel(const SelectParams p) {
   constexpr int kItems = 8, kWaves = NT / 64;

@@ -236,7 +236,7 @@ struct SelectParams {
   const int32_t *block_tables, *prefix_lens;
   int32_t *blocks, *count;    // [B, gamma, groups, Hkv, max_sel], [B, gamma, groups, Hkv]
   float *score;               // workspace [B * gamma * groups * Hkv, n_max]: rounded scores
-  float *top;                 // workspace [B * Hkv, n_tiles]: largest magnitude of 32 blocks' bounds
+  float *top;                 // workspace [B * Hkv, n_tiles]: largest magnitude of top_blocks blocks' bounds (32 or 64)
   double *exact;              // workspace [B * gamma * groups * Hkv, n_max]: scores in fp64 where a decision needs them
   int B, Hq, Hkv, G, D, gamma, L, group_len, n_groups, block_shift, max_blocks;
   int max_sel, keep_first, keep_last;
@@ -251,7 +251,7 @@ int block_pick_threads(int n_max, int rows);
 
 // Attention over selected blocks (sel == null: all blocks of the prefix).  A unit is one (request, group, KV head, tile of
 // the group's rows); without a selection one group holds the rows of all branches.  Its keys, the selected prefix rows and
-// then the branch-private tokens, are dealt out in tiles of 32 over n_split workgroups.
+// then the branch-private tokens, are dealt out in tiles of 32 or 64 (the kernel shape's) over n_split workgroups.
 struct SparseParams {
   const void *q, *k_cache, *v_cache, *k_branch, *v_branch;
   const uint8_t *k_exp, *v_exp;
